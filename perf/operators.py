@@ -4,7 +4,7 @@ Kinds of call (`kind`):
   embed   hidden states of a batch's input tokens, looked up in the table [V, d] and scaled; masked positions are zero
   grad    the table's gradient from the gradient of those states: rows of the same token are added up, into a fresh gradient or
           (`accumulate`) into the one that the loss step left in the tied head
-  quant   the table to 8 bits (e4m3) with a power of two as the scale of every 128 values of a row; stored [V, d] ("vd") or [d, V] ("dv")
+  quant   the table to 8 bits (e4m3) with a power of two as the scale of every 128 values of a row; given as [V, d] ("vd") or [d, V] ("dv")
   score   log-probs of sampled tokens under a policy whose head is kept in 8 bits
 
 A batch is N generations with lengths uniform in [len_lo, len_hi], padded to len_hi; with `holes` a fifth of the valid positions is masked too.
@@ -122,7 +122,12 @@ def prepare(case, seed):
         return s
     # hidden states as the final norm leaves them
     values, exponents = _to_8_bits(_table(case, gen).float())
-    return dict(s, hidden=_randn(shape, gen, 1.0, case["dtype"]), values=values, scales=(exponents + 127).to(torch.uint8))
+    return dict(s, hidden=_randn(shape, gen, 1.0, case["dtype"]), values=values, scales=_scales(exponents))
+
+
+def _scales(exponents):
+    """Scales as the head keeps them: a byte e + 127 a block, and whole words a row."""
+    return torch.nn.functional.pad((exponents + 127).to(torch.uint8), (0, -exponents.shape[1] % 4), value=127)
 
 
 def _power(e):
@@ -168,7 +173,7 @@ def _run_plain(s):
     if case["kind"] == "quant":
         W = s["W"].t() if case["layout"] == "dv" else s["W"]
         values, exponents = _to_8_bits(W.float())
-        return dict(values=values, scales=(exponents + 127).to(torch.uint8))
+        return dict(values=values, scales=_scales(exponents))
     valid = s["mask"].bool()
     tokens = s["tokens"][valid].long()
     if case["kind"] == "embed":
@@ -180,7 +185,7 @@ def _run_plain(s):
         if case["accumulate"]:
             return s["dtable"].index_add_(0, tokens, rows)
         return torch.zeros(s["dtable"].shape, device="cuda").index_add_(0, tokens, rows).to(s["dtable"].dtype)
-    W = _from_8_bits(s["values"], s["scales"].int() - 127)
+    W = _from_8_bits(s["values"], s["scales"][:, :s["values"].shape[1] // 128].int() - 127)
     h = _from_8_bits(*_to_8_bits(s["hidden"][valid].float()))
     z = (h @ W.t()) / case["temp"]
     zy = z.gather(1, tokens[:, None])[:, 0]
@@ -219,7 +224,8 @@ def exact(case, seed):
         for part in W.split(8192):
             q, e = _blocks64(part.double())
             values.append(q.view(part.shape[0], -1).float())
-            scales.append((e + 127).to(torch.uint8))
+            scales.append(torch.full((part.shape[0], -(-e.shape[1] // 4) * 4), 127, dtype=torch.uint8, device="cuda"))
+            scales[-1][:, :e.shape[1]] = (e + 127).to(torch.uint8)
         return dict(values=torch.cat(values).double(), scales=torch.cat(scales))
     N, T, d = case["N"], case["len_hi"], case["d"]
     where = s["mask"].reshape(-1).nonzero()[:, 0]
@@ -235,7 +241,8 @@ def exact(case, seed):
         for at, tok in zip(where.split(65536), tokens.split(65536)):
             out.index_add_(0, tok, flat[at].double() * case["scale"])
         return out
-    W = s["values"].double().view(case["V"], -1, 128) * torch.exp2(s["scales"].double() - 127)[:, :, None]
+    W = s["values"].double().view(case["V"], -1, 128)
+    W = W * torch.exp2(s["scales"][:, :W.shape[1]].double() - 127)[:, :, None]
     W = W.view(case["V"], -1)
     flat = s["hidden"].view(N * T, d)
     logp, lse = (torch.zeros(N * T, dtype=torch.float64, device="cuda") for _ in range(2))
@@ -259,7 +266,8 @@ def _distinct(case):
 
 def work(case):
     d, V, e = case["d"], case["V"], 2 if case["dtype"] == "bf16" else 4
-    in_8_bits = V * -(-d // 128) * 129
+    blocks = -(-d // 128)
+    in_8_bits = V * (blocks * 128 + -(-blocks // 4) * 4)
     if case["kind"] == "quant":     # the table in, values and scales out
         return dict(bytes=V * d * e + in_8_bits, flops=3 * V * d)
     M, positions = _tokens(case), case["N"] * case["len_hi"]
