@@ -67,6 +67,10 @@ extern "C" {
                                       call's outputs are not usable.  Repeat the call with logits_cache = 0, or with
                                       the workspace of rapid_workspace_bytes_max_tokens (one chunk, any layout) */
 
+#define RAPID_STATUS_NONFINITE_VALUE 128 /* 8-bit rows: an element of W (rapid_quantize_fp8) or of a valid hidden row
+                                      (rapid_logprob_fwd_fp8) is not finite.  It is stored as NaN, so the log-probs it
+                                      enters are not finite either */
+
 /* enums */
 #define RAPID_DTYPE_F32 0
 #define RAPID_DTYPE_BF16 1
@@ -76,6 +80,9 @@ extern "C" {
 #define RAPID_OP_GROUP_ADVANTAGE 1
 #define RAPID_OP_IW_PG_FWD_BWD 2
 #define RAPID_OP_IW_PG_FWD_BWD_CACHED 3 /* workspace query only: rapid_iw_pg_loss_fwd_bwd with logits_cache = 1 */
+
+#define RAPID_OP_EMBEDDING_BWD 4        /* rapid_embedding_bwd */
+#define RAPID_OP_LOGPROB_FWD_FP8 5      /* rapid_logprob_fwd_fp8 */
 
 /* Options of rapid_iw_pg_loss_fwd_bwd (host struct).  rapid_iw_pg_default_opts() fills the
  * paper's defaults: eta = 2.0 (Appendix A, RL hyper-parameter table), everything else as
@@ -159,7 +166,8 @@ void rapid_iw_pg_default_opts(rapid_iw_pg_opts* opts);
 /* Workspace sizes in bytes for `op` at the given problem size.  rapid_workspace_bytes is the
  * recommended size (backward row-chunks large enough to fill the chip); rapid_workspace_min_bytes
  * the smallest the call accepts (smaller chunks, same results).  RAPID_OP_GROUP_ADVANTAGE needs
- * none (returns 0).  RAPID_OP_IW_PG_FWD_BWD_CACHED are the sizes for rapid_iw_pg_loss_fwd_bwd with
+ * none (returns 0).  RAPID_OP_EMBEDDING_BWD and RAPID_OP_LOGPROB_FWD_FP8 have one size, which both return (K is not
+ * looked at).  RAPID_OP_IW_PG_FWD_BWD_CACHED are the sizes for rapid_iw_pg_loss_fwd_bwd with
  * opts->logits_cache = 1 (bf16 only): recommended = a cache of 90112 token rows (or of all N * T positions
  * if those are fewer), minimum = a cache of 256 rows; the call uses as many cache rows as the workspace
  * it is given affords.  rapid_workspace_bytes_max_tokens (cached op only; the others ignore the bound) is
@@ -341,6 +349,62 @@ int rapid_sgd_step(float* master, const float* grad, int64_t n, float lr, void* 
 int rapid_adamw_step(float* master, const float* grad, float* exp_avg, float* exp_avg_sq, int64_t n, float lr,
                      float beta1, float beta2, float eps, float weight_decay, int64_t step, void* w_out, int dtype,
                      void* stream);
+
+/*
+ * The head's other uses in a model that ties it to the input embedding: one table [V,d] (a head stored RAPID_W_VD).  An
+ * update of such a model is rapid_embedding_fwd, the model's body, rapid_iw_pg_loss_fwd_bwd (dW [V,d] fp32), the body's
+ * backward, rapid_embedding_bwd with accumulate = 1 into that dW, and an optimiser step.  None of this is part of the
+ * paper's method, whose path starts at the final hidden state.
+ *
+ *   hidden_out[n,t,:] = scale * table[tokens[n,t],:], rounded once     (zeros where mask = 0)
+ *
+ * table and hidden_out in `dtype`, 16-byte aligned (bf16: d % 8 == 0); mask may be NULL (every position valid).  A token id
+ * outside [0,V) at a valid position sets RAPID_STATUS_BAD_TOKEN; its row is zeros, and adds nothing to the gradient.
+ */
+int rapid_embedding_fwd(const void* table, const int32_t* tokens, const uint8_t* mask, int64_t N, int64_t T,
+                        int64_t d, int64_t V, int dtype, float scale, void* hidden_out, int32_t* dev_status,
+                        void* stream);
+
+/*
+ * Gradient of that lookup:
+ *   dtable_out[v,:] = scale * sum of dhidden[n,t,:] over the valid positions with tokens[n,t] = v     (accumulate = 0)
+ *   dtable_out[v,:] += the same; rows of ids that do not occur are not touched                        (accumulate = 1)
+ * dhidden in `dtype` (masked positions are not read), dtable_out in dw_dtype (accumulate: fp32 only), both 16-byte aligned.
+ * Sums are fp32, in an order that depends on the positions of an id and on N * T alone: the same inputs give the same bits.
+ * Workspace: rapid_workspace_bytes(RAPID_OP_EMBEDDING_BWD, N, T, d, V, ., dtype).
+ */
+int rapid_embedding_bwd(const void* dhidden, const int32_t* tokens, const uint8_t* mask, int64_t N, int64_t T,
+                        int64_t d, int64_t V, int dtype, float scale, int dw_dtype, int accumulate, void* dtable_out,
+                        int32_t* dev_status, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * A head in 8 bits, for policies that only score (the behaviour policy mu, the reference policy of the KL term): half the
+ * bytes and twice the matrix rate of bf16.  Row v of the head, W[v,0..d), is cut into blocks of 128; a block is stored as
+ * e4m3 values W * 2^-e (rounded once, to nearest even) and the E8M0 byte e + 127, with e the smallest integer >= -126 for
+ * which the block's largest magnitude is <= 448 * 2^e (0 for a block of zeros).
+ *   values [V, rapid_fp8_value_bytes(d)]: d rounded up to whole blocks, zeros behind d; 16-byte aligned
+ *   scales [V, rapid_fp8_scale_bytes(d)]: the number of blocks rounded up to 4, 127 behind the last; 4-byte aligned
+ * W is in `dtype`, [d,V] or [V,d] by w_layout; what is written is the same for both.
+ */
+int64_t rapid_fp8_value_bytes(int64_t d);
+int64_t rapid_fp8_scale_bytes(int64_t d);
+int rapid_quantize_fp8(const void* W, int64_t d, int64_t V, int dtype, int w_layout, void* values_out,
+                       uint8_t* scales_out, int32_t* dev_status, void* stream);
+
+/*
+ * rapid_logprob_fwd under such a head.  The hidden rows (bf16 or fp32) are brought to 8 bits in the same way, in the call:
+ *   z = sum over blocks b of 2^(e_hidden[b] + e_W[v,b]) * <e4m3 values of block b> / temperature
+ *   logp_out[n,t] = z[y] - logsumexp(z) (at most 0), lse_out[n,t] = logsumexp(z) (may be NULL); 0 where mask = 0
+ * z[y] is summed in fp32.  The logits of the log-sum-exp come from the 8-bit matrix unit, which adds eight neighbouring products
+ * with the bits from 2^-13 of the largest on and everything else in fp32: about 1e-4 of the logits' spread, some
+ * hundredths of what the rounding to e4m3 moves them by.
+ * A token id outside [0,V) is treated as token 0 (RAPID_STATUS_BAD_TOKEN).  At most 2^25 positions.  Workspace:
+ * rapid_workspace_bytes(RAPID_OP_LOGPROB_FWD_FP8, N, T, d, V, ., dtype).
+ */
+int rapid_logprob_fwd_fp8(const void* hidden, const void* values, const uint8_t* scales, const int32_t* tokens,
+                          const uint8_t* mask, int64_t N, int64_t T, int64_t d, int64_t V, int dtype,
+                          float temperature, float* logp_out, float* lse_out, int32_t* dev_status, void* workspace,
+                          size_t workspace_bytes, void* stream);
 
 /*
  * Integer bookkeeping of the padding mask (device outputs; seq_len_out and cu_seqlen_out are

@@ -19,15 +19,18 @@ RAPID_OK = 0
 DTYPE_F32, DTYPE_BF16 = 0, 1
 W_DV, W_VD = 0, 1
 OP_LOGPROB_FWD, OP_GROUP_ADVANTAGE, OP_IW_PG_FWD_BWD, OP_IW_PG_FWD_BWD_CACHED = 0, 1, 2, 3
+OP_EMBEDDING_BWD, OP_LOGPROB_FWD_FP8 = 4, 5
 STATUS_BAD_TOKEN, STATUS_BAD_GROUP, STATUS_NONFINITE_REWARD, STATUS_NONFINITE_LOGP, STATUS_LOGIT_RANGE = 1, 2, 4, 8, 16
 STATUS_TOKEN_BOUND = 32
 STATUS_GROUP_LAYOUT = 64
+STATUS_NONFINITE_VALUE = 128
 
 EXPORTS = ["rapid_version", "rapid_last_error", "rapid_logits_cache_rows", "rapid_iw_pg_default_opts", "rapid_set_tuning",
            "rapid_workspace_bytes", "rapid_workspace_min_bytes", "rapid_workspace_bytes_max_tokens", "rapid_logprob_fwd", "rapid_logprob_fwd_rmsnorm",
            "rapid_group_advantage", "rapid_iw_pg_loss_fwd_bwd", "rapid_compaction", "rapid_profile_read", "rapid_mfma_probe", "rapid_sgd_step",
            "rapid_logprob_fwd_static", "rapid_clip_pg_default_opts", "rapid_clip_pg_loss_fwd_bwd",
-           "rapid_seq_logratio", "rapid_adamw_step"]
+           "rapid_seq_logratio", "rapid_adamw_step", "rapid_embedding_fwd", "rapid_embedding_bwd", "rapid_fp8_value_bytes",
+           "rapid_fp8_scale_bytes", "rapid_quantize_fp8", "rapid_logprob_fwd_fp8"]
 STAGES = ["compaction", "pack", "fwd_lse", "merge_lse", "estimator", "zero_rows", "dz", "unused", "dh",
           "dw", "f32_path", "dw_convert"]
 
@@ -117,6 +120,17 @@ def load():
     lib.rapid_adamw_step.restype = ci
     lib.rapid_seq_logratio.argtypes = [vp, vp, vp, i64, i64, vp, vp, vp, vp]
     lib.rapid_seq_logratio.restype = ci
+    lib.rapid_embedding_fwd.argtypes = [vp, vp, vp, i64, i64, i64, i64, ci, f32, vp, vp, vp]
+    lib.rapid_embedding_fwd.restype = ci
+    lib.rapid_embedding_bwd.argtypes = [vp, vp, vp, i64, i64, i64, i64, ci, f32, ci, ci, vp, vp, vp, sz, vp]
+    lib.rapid_embedding_bwd.restype = ci
+    for fn in (lib.rapid_fp8_value_bytes, lib.rapid_fp8_scale_bytes):
+        fn.argtypes = [i64]
+        fn.restype = i64
+    lib.rapid_quantize_fp8.argtypes = [vp, i64, i64, ci, ci, vp, vp, vp, vp]
+    lib.rapid_quantize_fp8.restype = ci
+    lib.rapid_logprob_fwd_fp8.argtypes = [vp, vp, vp, vp, vp, i64, i64, i64, i64, ci, f32, vp, vp, vp, vp, sz, vp]
+    lib.rapid_logprob_fwd_fp8.restype = ci
     _lib = lib
     return lib
 
@@ -155,6 +169,11 @@ def _dtype_code(t):
 def _need(t, dtype, name):
     if not t.is_cuda or not t.is_contiguous() or t.dtype != dtype:
         raise TypeError(f"{name}: need a contiguous {dtype} tensor on the GPU")
+
+
+def _shape(t, shape, name):
+    if tuple(t.shape) != tuple(shape):
+        raise TypeError(f"{name}: shape {tuple(t.shape)}, need {tuple(shape)}")
 
 
 def rapid_version():
@@ -282,6 +301,90 @@ def rapid_logprob_fwd_static(hidden, W, tokens, mask, logp_out, lse_out=None, w_
                                            float(temperature), _ptr(logp_out), _ptr(lse_out), _ptr(dev_status),
                                            _stream()))
     return logp_out, lse_out
+
+
+def rapid_embedding_fwd(table, tokens, mask=None, scale=1.0, out=None, dev_status=None):
+    """Returns hidden [N,T,d] = scale * table[tokens] (table [V,d]), zeros where mask is 0 (mask None: nowhere)."""
+    N, T = tokens.shape
+    V, d = table.shape
+    _need(table, table.dtype, "table"); _need(tokens, torch.int32, "tokens")
+    if mask is not None:
+        _need(mask, torch.uint8, "mask"); _shape(mask, (N, T), "mask")
+    if out is None:
+        out = torch.empty((N, T, d), dtype=table.dtype, device=table.device)
+    _need(out, table.dtype, "out"); _shape(out, (N, T, d), "out")
+    _check(load().rapid_embedding_fwd(_ptr(table), _ptr(tokens), _ptr(mask), N, T, d, V, _dtype_code(table), float(scale),
+                                      _ptr(out), _ptr(dev_status), _stream()))
+    return out
+
+
+def rapid_embedding_bwd(dhidden, tokens, mask, V, scale=1.0, dtable=None, dw_dtype=torch.float32, accumulate=False,
+                        workspace=None, dev_status=None):
+    """Gradient of rapid_embedding_fwd's table: returns dtable [V,d], a new tensor of dw_dtype or the one handed in
+    (overwritten, or with accumulate added to: the dW that a tied head's loss step left)."""
+    N, T, d = dhidden.shape
+    _need(dhidden, dhidden.dtype, "dhidden"); _need(tokens, torch.int32, "tokens"); _shape(tokens, (N, T), "tokens")
+    if mask is not None:
+        _need(mask, torch.uint8, "mask"); _shape(mask, (N, T), "mask")
+    dt = _dtype_code(dhidden)
+    if dtable is None:
+        if accumulate:
+            raise TypeError("accumulate needs the dtable to add to")
+        dtable = torch.empty((V, d), dtype=dw_dtype, device=dhidden.device)
+    _need(dtable, dtable.dtype, "dtable"); _shape(dtable, (V, d), "dtable")
+    if workspace is None:
+        workspace = alloc_workspace(rapid_workspace_bytes(OP_EMBEDDING_BWD, N, T, d, V, 1, dt), dhidden.device)
+    _check(load().rapid_embedding_bwd(_ptr(dhidden), _ptr(tokens), _ptr(mask), N, T, d, V, dt, float(scale),
+                                      _dtype_code(dtable), int(bool(accumulate)), _ptr(dtable), _ptr(dev_status),
+                                      _ptr(workspace), workspace.numel(), _stream()))
+    return dtable
+
+
+class Fp8Weight:
+    """A head in 8 bits: values [V, d up to whole blocks of 128] float8_e4m3fn, scales [V, blocks up to a multiple of 4] uint8
+    (E8M0: the scale of a block is 2^(byte - 127)), and d."""
+
+    def __init__(self, values, scales, d):
+        _need(values, torch.float8_e4m3fn, "values"); _need(scales, torch.uint8, "scales")
+        lib = load()
+        _shape(values, (values.shape[0], lib.rapid_fp8_value_bytes(d)), "values")
+        _shape(scales, (values.shape[0], lib.rapid_fp8_scale_bytes(d)), "scales")
+        self.values, self.scales, self.d = values, scales, d
+
+
+def rapid_quantize_fp8(W, w_layout=W_DV, out=None, dev_status=None):
+    """Returns W [d,V] or [V,d] (w_layout) as an Fp8Weight: a new one, or `out` filled in place."""
+    d, V = W.shape if w_layout == W_DV else W.shape[::-1]
+    _need(W, W.dtype, "W")
+    if out is None:
+        lib = load()
+        out = Fp8Weight(torch.empty((V, lib.rapid_fp8_value_bytes(d)), dtype=torch.float8_e4m3fn, device=W.device),
+                        torch.empty((V, lib.rapid_fp8_scale_bytes(d)), dtype=torch.uint8, device=W.device), d)
+    if out.d != d or out.values.shape[0] != V:
+        raise TypeError("out: another head's size")
+    _check(load().rapid_quantize_fp8(_ptr(W), d, V, _dtype_code(W), w_layout, _ptr(out.values), _ptr(out.scales),
+                                     _ptr(dev_status), _stream()))
+    return out
+
+
+def rapid_logprob_fwd_fp8(hidden, W8, tokens, mask, temperature=1.0, want_lse=False, workspace=None, dev_status=None):
+    """rapid_logprob_fwd under an Fp8Weight.  Returns (logp [N,T] f32, lse [N,T] f32 or None)."""
+    N, T, d = hidden.shape
+    V = W8.values.shape[0]
+    dt = _dtype_code(hidden)
+    if d != W8.d:
+        raise TypeError(f"hidden has {d} columns, the head {W8.d}")
+    _need(hidden, hidden.dtype, "hidden")
+    _need(tokens, torch.int32, "tokens"); _shape(tokens, (N, T), "tokens")
+    _need(mask, torch.uint8, "mask"); _shape(mask, (N, T), "mask")
+    if workspace is None:
+        workspace = alloc_workspace(rapid_workspace_bytes(OP_LOGPROB_FWD_FP8, N, T, d, V, 1, dt), hidden.device)
+    logp = torch.empty((N, T), dtype=torch.float32, device=hidden.device)
+    lse = torch.empty((N, T), dtype=torch.float32, device=hidden.device) if want_lse else None
+    _check(load().rapid_logprob_fwd_fp8(_ptr(hidden), _ptr(W8.values), _ptr(W8.scales), _ptr(tokens), _ptr(mask), N, T, d, V, dt,
+                                        float(temperature), _ptr(logp), _ptr(lse), _ptr(dev_status), _ptr(workspace),
+                                        workspace.numel(), _stream()))
+    return logp, lse
 
 
 def rapid_group_advantage(rewards, group_ids, K, seq_logratio=None, eta=2.0, baseline_mode=0,

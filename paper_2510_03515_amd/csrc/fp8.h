@@ -1,0 +1,90 @@
+// 8-bit rows: e4m3 values with a power of two as the scale of every block of 128.
+//
+// Block exponent e: the smallest integer >= -126 with (largest finite magnitude of the block) <= 448 2^e; 0 for a block of zeros.  The
+// stored value is x 2^-e rounded to e4m3 once, to nearest even (448 is the largest e4m3 value, so nothing saturates; the product with a power
+// of two is exact).  A value that is not finite is stored as NaN.  Scales are kept as E8M0 bytes, e + 127: what the scaled MFMA takes.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "row_math.h"
+
+namespace rapid {
+
+constexpr int FP8_BLOCK = 128;
+// bytes of a row of values, and of its scales (whole 32-bit words, for loads of four)
+__host__ __device__ inline int64_t fp8_row(int64_t d) { return (d + FP8_BLOCK - 1) / FP8_BLOCK * FP8_BLOCK; }
+__host__ __device__ inline int64_t fp8_scale_row(int64_t d) { return (fp8_row(d) / FP8_BLOCK + 3) / 4 * 4; }
+
+__device__ __forceinline__ uint32_t finite_magnitude(float x) {
+    const uint32_t b = __builtin_bit_cast(uint32_t, x) & 0x7fffffffu;
+    return b < 0x7f800000u ? b : 0u;
+}
+// E8M0 byte of a block whose largest finite magnitude has the bits `most` (1.75 2^8 = 448)
+__device__ __forceinline__ uint32_t block_scale(uint32_t most) {
+    if (most == 0u) return 127u;
+    const int e = (int)(most >> 23) - 8 + ((most & 0x7fffffu) > 0x600000u ? 1 : 0);
+    return (uint32_t)(e < 1 ? 1 : e);
+}
+__device__ __forceinline__ float scale_inverse(uint32_t byte) { return __builtin_bit_cast(float, (254u - byte) << 23); }
+__device__ __forceinline__ float scale_value(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
+
+// 4 values, scaled and rounded
+__device__ __forceinline__ uint32_t to_fp8x4(float a, float b, float c, float d, float inverse) {
+    int v = 0;
+    v = __builtin_amdgcn_cvt_pk_fp8_f32(a * inverse, b * inverse, v, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c * inverse, d * inverse, v, true);
+}
+__device__ __forceinline__ float not_finite_is_nan(float x, bool& bad) {
+    const bool ok = (__builtin_bit_cast(uint32_t, x) & 0x7f800000u) != 0x7f800000u;
+    bad |= !ok;
+    return ok ? x : __builtin_nanf("");
+}
+__device__ __forceinline__ void from_fp8x4(uint32_t v, float (&f)[4]) {
+    f[0] = __builtin_amdgcn_cvt_f32_fp8((int)v, 0);
+    f[1] = __builtin_amdgcn_cvt_f32_fp8((int)v, 1);
+    f[2] = __builtin_amdgcn_cvt_f32_fp8((int)v, 2);
+    f[3] = __builtin_amdgcn_cvt_f32_fp8((int)v, 3);
+}
+
+__device__ __forceinline__ float to_float(float x) { return x; }
+__device__ __forceinline__ float to_float(unsigned short x) { return __builtin_bit_cast(float, (uint32_t)x << 16); }
+
+// 8 consecutive elements from column c on of a row of d: bf16 (d % 8 == 0) or fp32; zeros behind the end
+__device__ __forceinline__ void load8(const unsigned short* row, int64_t c, int64_t d, float (&x)[8]) {
+    uint4 v = make_uint4(0u, 0u, 0u, 0u);
+    if (c < d) v = *(const uint4*)(row + c);
+    unpack8(v, x);
+}
+__device__ __forceinline__ void load8(const float* row, int64_t c, int64_t d, float (&x)[8]) {
+    if (d % 4 == 0) {
+        float4 a = make_float4(0.f, 0.f, 0.f, 0.f), b = a;
+        if (c < d) a = *(const float4*)(row + c);
+        if (c + 4 < d) b = *(const float4*)(row + c + 4);
+        x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w; x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = c + e < d ? row[c + e] : 0.f;
+    }
+}
+// the block that 16 lanes hold 8 elements each of: its scale, and the lane's elements rounded
+__device__ __forceinline__ uint2 quantize_block(float (&x)[8], uint32_t& scale, bool& bad) {
+    uint32_t most = 0u;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) most = max(most, finite_magnitude(x[e]));
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, o, 64));
+    scale = block_scale(most);
+    const float inv = scale_inverse(scale);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = not_finite_is_nan(x[e], bad);
+    return make_uint2(to_fp8x4(x[0], x[1], x[2], x[3], inv), to_fp8x4(x[4], x[5], x[6], x[7], inv));
+}
+
+// the scales of the four blocks that a wave holds, as a word
+__device__ __forceinline__ uint32_t scale_word(uint32_t s) {
+    return (uint32_t)__shfl((int)s, 0, 64) | (uint32_t)__shfl((int)s, 16, 64) << 8 | (uint32_t)__shfl((int)s, 32, 64) << 16 |
+           (uint32_t)__shfl((int)s, 48, 64) << 24;
+}
+
+}  // namespace rapid

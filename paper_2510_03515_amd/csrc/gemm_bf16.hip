@@ -33,6 +33,7 @@
 #include <type_traits>
 #include <utility>
 
+#include "mfma_tiles.h"
 #include "rapid_internal.h"
 
 namespace rapid {
@@ -41,50 +42,14 @@ namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
-
-constexpr float LOG2E = 1.4426950408889634f;
-
-// Geometry of a workgroup: NWI x NWJ waves, each owning WI x WJ blocks of 32 x 32.
-// 2 x 4 waves of 128 x 64 is the default (two waves per SIMD, which lets the hardware overlap one
-// wave's LDS, barrier and memory-issue waits with the other's MFMAs at the price of 1.5x the LDS
-// fragment reads); 2 x 2 waves of 128 x 128 (one wave per SIMD, 256 accumulator registers per lane)
-// and 2 x 8 waves of 128 x 32 are selectable.
-template <int NWI_, int NWJ_, int WI_, int WJ_>
-struct Geo {
-    static constexpr int NWI = NWI_, NWJ = NWJ_, WI = WI_, WJ = WJ_;
-    static constexpr int NW = NWI * NWJ, NT = 64 * NW;
-    static constexpr int BI = NWI * WI * 32, BJ = NWJ * WJ * 32;
-    // A k-major operand of 192 (or 224) columns is loaded as 256 (a request then covers whole rows; the last columns are
-    // not used), so an LDS stage has room for a power of two.
-    static constexpr int LI = BI > 128 ? 256 : BI, LJ = BJ > 128 ? 256 : BJ;
-    static constexpr int STAGE_BYTES = (LI + LJ) * 128;
-    static constexpr int LDS_BYTES = 2 * STAGE_BYTES;
-};
-
-// Barrier without the memory fence of __syncthreads; the loops place their own waits before it.
-__device__ __forceinline__ void lds_barrier() {
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-}
 
 template <int WI, int WJ>
 struct Frags {
     bf16x8 a[WI], b[WJ];
 };
 
-// LDS fragment reads and their waits are issued by hand.  With direct memory -> LDS loads in the
-// loop the compiler's wait insertion falls back to lgkmcnt(0) before every MFMA block, which also
-// waits for the reads just issued for the NEXT sub-step and so undoes the software pipelining.
-// LDS reads of a wave complete in order, so "at most n reads outstanding" after issuing the next
-// sub-step's n reads means exactly "the current sub-step's fragments have arrived".
-__device__ __forceinline__ uint32_t lds_addr(const char* p) {
-    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p;
-}
 template <int OFF>
 __device__ __forceinline__ bf16x8 ds_read128(uint32_t addr) {
     bf16x8 v;
@@ -152,16 +117,6 @@ __device__ __forceinline__ void request_first_half(F&& request) {
     for (int r = 0; r < T; ++r)
         if (r * 2 * NB / T < NB) request(r);
 }
-__device__ __forceinline__ void load_to_lds_16(const char* gp, char* lp) {
-    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)gp,
-                                     (__attribute__((address_space(3))) void*)lp, 16, 0, 0);
-}
-
-// Scheduling fence: nothing is moved across it.  The K step is written in the order that software-
-// pipelines it (fragments of the next sub-step are requested before the MFMAs of the current one,
-// tile requests sit between given MFMAs) and the fences keep that order.
-__device__ __forceinline__ void fence() { __builtin_amdgcn_sched_barrier(0); }
-
 struct NoPace {
     __device__ __forceinline__ void operator()(int) const {}
 };
@@ -741,31 +696,11 @@ __device__ __forceinline__ void mainloop_kmajor32(const bf16_t* __restrict__ A, 
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");   // the requests for steps that do not exist
 }
 
-// Workgroup id -> tile.  Hardware deals consecutive workgroup ids round-robin to the 8 XCDs (each
-// with its own L2), so id % 8 picks the XCD and id / 8 the position in that XCD's contiguous share
-// of a grouped order: GI tiles along i for one j, then the next j, ... so that workgroups resident
-// together on an XCD re-use each other's operand panels out of L2.
-struct TileId { int ti, tj; bool valid; };
-// position `vid` of the grouped order -> tile
-__device__ __forceinline__ TileId tile_of_vid(int vid, int tilesI, int tilesJ, int GI) {
-    const int total = tilesI * tilesJ;
-    TileId t;
-    t.valid = vid < total;
-    const int group_sz = GI * tilesJ;
-    const int grp = vid / group_sz;
-    const int first_i = grp * GI;
-    const int gi = min(GI, tilesI - first_i);
-    const int rem = vid - grp * group_sz;
-    t.ti = first_i + rem % gi;
-    t.tj = rem / gi;
-    return t;
-}
 __device__ __forceinline__ TileId map_tile(int pid, int tilesI, int tilesJ, int GI) {
     const int per = (tilesI * tilesJ + 7) / 8;
     return tile_of_vid((pid & 7) * per + (pid >> 3), tilesI, tilesJ, GI);
 }
 
-__host__ __device__ inline int ids_for(int tilesI, int tilesJ) { return (int)(((int64_t)tilesI * tilesJ + 7) / 8 * 8); }
 // The kernels are persistent: one workgroup per CU (LDS admits no more) walks the ids
 // blockIdx.x, blockIdx.x + gridDim.x, ...; gridDim.x is a multiple of 8, so a workgroup stays on its
 // XCD's share of the order and the workgroups of an XCD stay on neighbouring tiles.  This saves the
@@ -792,19 +727,6 @@ __device__ __forceinline__ Operand dh_w(const WInPlace& w, int ti, int k0) {
     if (WM == W_VD) return Operand{w.W + v0 * w.d + d0, w.d, w.d * (K_TILE * 2), (int)(w.d - d0), w.V - v0};
     return Operand{w.W + d0 * w.V + v0, w.V, 128, (int)(w.d - d0), w.V - v0};
 }
-
-template <class S>
-struct Lane {
-    int lane, wave, wave_i, wave_j, hi, lj;
-    __device__ __forceinline__ Lane() {
-        lane = threadIdx.x & 63;
-        wave = threadIdx.x >> 6;
-        wave_i = wave % S::NWI;
-        wave_j = wave / S::NWI;
-        hi = lane >> 5;
-        lj = lane & 31;
-    }
-};
 
 __device__ __forceinline__ uint2 pack_bf16x4(float a, float b, float c, float d) {
     bf16x4 r;
@@ -850,21 +772,6 @@ __device__ __forceinline__ void store_tile_through_lds(char* lds, const Lane<S>&
         for (int tt = 0; tt < 8; ++tt)
             __builtin_nontemporal_store(__builtin_bit_cast(u32x4, v[tt]), (u32x4*)(o + (int64_t)(jb * 8 + tt) * 4 * ld));
     }
-}
-
-// ragged last vocabulary tile: the columns that do not exist become -infinity
-template <class S>
-__device__ __forceinline__ void mask_padding(f32x16 (&acc)[S::WI][S::WJ], int n_valid, int hi) {
-    if (n_valid >= S::WI * 32) return;
-#pragma unroll
-    for (int ib = 0; ib < S::WI; ++ib)
-#pragma unroll
-        for (int jb = 0; jb < S::WJ; ++jb)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const int rel = ib * 32 + (v >> 2) * 8 + hi * 4 + (v & 3);
-                acc[ib][jb][v] = rel < n_valid ? acc[ib][jb][v] : -INFINITY;
-            }
 }
 
 // ------------------------------------------------------------------------------------- fwd_lse
@@ -1685,19 +1592,6 @@ __global__ __launch_bounds__(256) void cache_finish_kernel(bf16_t* __restrict__ 
     }
 }
 
-// Lets `kernel` use `bytes` of dynamic LDS: once per kernel and device (the attribute belongs to the
-// device's copy of the function), not once per launch.  One static bit mask per kernel.
-template <auto kernel>
-void allow_lds(int bytes) {
-    static std::atomic<uint64_t> done{0};
-    int dev = 0;
-    (void)hipGetDevice(&dev);
-    const uint64_t bit = 1ull << (dev & 63);
-    if (done.load(std::memory_order_acquire) & bit) return;
-    if (hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess)
-        done.fetch_or(bit, std::memory_order_release);
-}
-
 // waves per workgroup: 4 (2 x 2 of 128 x 128), 8 (2 x 4 of 128 x 64) or 16; 0 = each kernel's own
 // default: 8 for the logits kernels and dW, 4 for dHidden (measured: its long K loop gains more from
 // the 4-wave tile's third fewer LDS reads than it loses in latency hiding)
@@ -1774,6 +1668,7 @@ size_t dh_part_bytes() { return (size_t)MAX_UNITS * 256 * 256 * 4; }
 bool default_waves() { return g_waves.load() == 0; }
 void set_waves_per_workgroup(int n) { g_waves = (n == 4 || n == 8 || n == 16) ? n : 0; }
 void set_cu_count(int n) { g_num_cu = n >= 8 ? n : 8; }
+int cu_count() { return g_num_cu.load(); }
 
 
 void launch_block_w32(const bf16_t* Wvd, int64_t ldk, bf16_t* out, int64_t Vpad, int64_t dpad, hipStream_t st) {

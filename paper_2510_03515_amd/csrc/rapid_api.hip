@@ -8,6 +8,7 @@
 #include <cmath>
 #include <mutex>
 
+#include "fp8.h"
 #include "rapid_internal.h"
 #include "rapid_tuning.h"
 
@@ -363,6 +364,12 @@ int check_launch(const char* what) {
     return RAPID_OK;
 }
 
+// limits of the calls on a table (those of make_plan)
+bool table_shape(int64_t N, int64_t T, int64_t d, int64_t V) {
+    return N > 0 && T > 0 && d > 0 && V > 0 && N <= (int64_t)2000000000 && T <= (int64_t)2000000000 && N * T <= (int64_t)2000000000 &&
+           V <= (int64_t)4000000 && d <= 65536;
+}
+
 template <class T>
 T* at(void* ws, size_t off) { return (T*)((char*)ws + off); }
 
@@ -653,6 +660,66 @@ int logprob_fwd(const void* hidden, const void* W, const int32_t* tokens, const 
     return check_launch("rapid_logprob_fwd");
 }
 
+// Workspace of rapid_logprob_fwd_fp8
+struct Fp8Plan {
+    int64_t Mpad, ld8;
+    int tilesV;
+    size_t counts, seq_len, cu, row_index, tokc, seqc, zy, lse_c, h_scales, H8, part_max, part_sum, total;
+};
+bool make_fp8_plan(Fp8Plan& p, int64_t N, int64_t T, int64_t d, int64_t V) {
+    if (!table_shape(N, T, d, V) || N * T > ((int64_t)1 << 25)) return false;      // a launch holds less than 2^32 threads, 64 a row
+    p.Mpad = round_up(N * T, ROW_TILE);
+    p.ld8 = padded_ld(fp8_row(d) / 2) * 2;
+    p.tilesV = (int)((V + 255) / 256);
+    size_t cur = 0;
+    p.counts = take(cur, CNT_WORDS * 4);
+    p.seq_len = take(cur, (size_t)N * 4);
+    p.cu = take(cur, (size_t)(N + 1) * 4);
+    p.row_index = take(cur, (size_t)p.Mpad * 4);
+    p.tokc = take(cur, (size_t)p.Mpad * 4);
+    p.seqc = take(cur, (size_t)p.Mpad * 4);
+    p.zy = take(cur, (size_t)p.Mpad * 4);
+    p.lse_c = take(cur, (size_t)p.Mpad * 4);
+    p.h_scales = take(cur, (size_t)p.Mpad * fp8_scale_row(d));
+    p.H8 = take(cur, (size_t)p.Mpad * p.ld8);
+    p.part_max = take(cur, (size_t)p.tilesV * fwd_slots_per_tile() * p.Mpad * 4);
+    p.part_sum = take(cur, (size_t)p.tilesV * fwd_slots_per_tile() * p.Mpad * 4);
+    p.total = cur;
+    return true;
+}
+
+int validate_table(const char* what, int64_t N, int64_t T, int64_t d, int64_t V, int dtype, const void* a, const void* b) {
+    if (dtype != RAPID_DTYPE_F32 && dtype != RAPID_DTYPE_BF16) {
+        set_error("%s: unknown dtype %d", what, dtype);
+        return RAPID_ERR_DTYPE;
+    }
+    if (!table_shape(N, T, d, V) || (dtype == RAPID_DTYPE_BF16 && d % 8 != 0)) {
+        set_error("%s: bad shape N=%lld T=%lld d=%lld V=%lld (bf16 needs d %% 8 == 0)", what, (long long)N, (long long)T, (long long)d, (long long)V);
+        return RAPID_ERR_SHAPE;
+    }
+    if (((uintptr_t)a | (uintptr_t)b) % 16 != 0) {
+        set_error("%s: tables and hidden states must be 16-byte aligned", what);
+        return RAPID_ERR_SHAPE;
+    }
+    return RAPID_OK;
+}
+int validate_workspace(const char* what, const void* workspace, size_t bytes, size_t need) {
+    if (!workspace || ((uintptr_t)workspace) % 256 != 0) {
+        set_error("workspace must be non-NULL and 256-byte aligned");
+        return RAPID_ERR_WORKSPACE;
+    }
+    if (bytes < need) {
+        set_error("%s: workspace of %zu bytes is below the minimum %zu", what, bytes, need);
+        return RAPID_ERR_WORKSPACE;
+    }
+    return RAPID_OK;
+}
+int validate_scale(const char* what, float scale) {
+    if (std::isfinite(scale)) return RAPID_OK;
+    set_error("%s: scale must be finite", what);
+    return RAPID_ERR_SHAPE;
+}
+
 }  // namespace
 }  // namespace rapid
 
@@ -660,7 +727,7 @@ using namespace rapid;
 
 extern "C" {
 
-int rapid_version(void) { return 7; }
+int rapid_version(void) { return 8; }
 
 const char* rapid_last_error(void) { return g_err; }
 
@@ -858,8 +925,17 @@ int64_t rapid_logits_cache_rows(int64_t N, int64_t T, int64_t d, int64_t V, int6
     return choose_cache(N, T, d, V, K, cache_rows(p, max_tokens), workspace_bytes, &p);
 }
 
+// calls whose workspace has one size
+static size_t one_size_workspace(int op, int64_t N, int64_t T, int64_t d, int64_t V, int dtype) {
+    if ((dtype != RAPID_DTYPE_F32 && dtype != RAPID_DTYPE_BF16) || !table_shape(N, T, d, V)) return 0;
+    if (op == RAPID_OP_EMBEDDING_BWD) return embedding_plan(N * T, d, V).total;
+    Fp8Plan p;
+    return make_fp8_plan(p, N, T, d, V) ? p.total : 0;
+}
+
 size_t rapid_workspace_bytes(int op, int64_t N, int64_t T, int64_t d, int64_t V, int64_t K, int dtype) {
     if (op == RAPID_OP_GROUP_ADVANTAGE) return 0;
+    if (op == RAPID_OP_EMBEDDING_BWD || op == RAPID_OP_LOGPROB_FWD_FP8) return one_size_workspace(op, N, T, d, V, dtype);
     Plan p;
     if (op == RAPID_OP_IW_PG_FWD_BWD_CACHED) {   // a cache of the recommended number of rows, or of all rows if those are fewer
         if (dtype != RAPID_DTYPE_BF16 || !make_plan(p, RAPID_OP_IW_PG_FWD_BWD, N, T, d, V, K, dtype)) return 0;
@@ -873,6 +949,7 @@ size_t rapid_workspace_bytes(int op, int64_t N, int64_t T, int64_t d, int64_t V,
 
 size_t rapid_workspace_min_bytes(int op, int64_t N, int64_t T, int64_t d, int64_t V, int64_t K, int dtype) {
     if (op == RAPID_OP_GROUP_ADVANTAGE) return 0;
+    if (op == RAPID_OP_EMBEDDING_BWD || op == RAPID_OP_LOGPROB_FWD_FP8) return one_size_workspace(op, N, T, d, V, dtype);
     Plan p;
     size_t least = 0;
     for (const bool any_tile : {true, false}) {
@@ -952,6 +1029,133 @@ int rapid_logprob_fwd_rmsnorm(const void* hidden, const void* W, const int32_t* 
     }
     return logprob_fwd(hidden, W, tokens, mask, N, T, d, V, dtype, w_layout, temperature, rms_weight, rms_eps,
                        logp_out, lse_out, dev_status, workspace, workspace_bytes, stream);
+}
+
+int rapid_embedding_fwd(const void* table, const int32_t* tokens, const uint8_t* mask, int64_t N, int64_t T, int64_t d, int64_t V,
+                        int dtype, float scale, void* hidden_out, int32_t* dev_status, void* stream) {
+    if (!table || !tokens || !hidden_out) {
+        set_error("table, tokens and hidden_out must not be NULL");
+        return RAPID_ERR_NULL;
+    }
+    int rc = validate_table("rapid_embedding_fwd", N, T, d, V, dtype, table, hidden_out);
+    if (!rc) rc = validate_scale("rapid_embedding_fwd", scale);
+    if (!rc) rc = check_arch();
+    if (rc) return rc;
+    EmbeddingArgs a;
+    a.tokens = tokens; a.mask = mask; a.positions = N * T; a.d = d; a.V = V; a.dtype = dtype; a.scale = scale; a.dev_status = dev_status;
+    launch_embedding_fwd(a, table, hidden_out, (hipStream_t)stream);
+    return check_launch("rapid_embedding_fwd");
+}
+
+int rapid_embedding_bwd(const void* dhidden, const int32_t* tokens, const uint8_t* mask, int64_t N, int64_t T, int64_t d, int64_t V,
+                        int dtype, float scale, int dw_dtype, int accumulate, void* dtable_out, int32_t* dev_status, void* workspace,
+                        size_t workspace_bytes, void* stream) {
+    if (!dhidden || !tokens || !dtable_out) {
+        set_error("dhidden, tokens and dtable_out must not be NULL");
+        return RAPID_ERR_NULL;
+    }
+    int rc = validate_table("rapid_embedding_bwd", N, T, d, V, dtype, dhidden, dtable_out);
+    if (!rc) rc = validate_scale("rapid_embedding_bwd", scale);
+    if (rc) return rc;
+    if ((dw_dtype != RAPID_DTYPE_F32 && dw_dtype != RAPID_DTYPE_BF16) || (accumulate && dw_dtype != RAPID_DTYPE_F32)) {
+        set_error("rapid_embedding_bwd: dw_dtype %d (a gradient is added to in fp32 only)", dw_dtype);
+        return RAPID_ERR_DTYPE;
+    }
+    const EmbeddingPlan p = embedding_plan(N * T, d, V);
+    rc = validate_workspace("rapid_embedding_bwd", workspace, workspace_bytes, p.total);
+    if (!rc) rc = check_arch();
+    if (rc) return rc;
+    EmbeddingArgs a;
+    a.tokens = tokens; a.mask = mask; a.positions = N * T; a.d = d; a.V = V; a.dtype = dtype; a.scale = scale; a.dev_status = dev_status;
+    launch_embedding_bwd(a, p, workspace, dhidden, dw_dtype, accumulate != 0, dtable_out, (hipStream_t)stream);
+    return check_launch("rapid_embedding_bwd");
+}
+
+int64_t rapid_fp8_value_bytes(int64_t d) { return d > 0 ? fp8_row(d) : 0; }
+int64_t rapid_fp8_scale_bytes(int64_t d) { return d > 0 ? fp8_scale_row(d) : 0; }
+
+int rapid_quantize_fp8(const void* W, int64_t d, int64_t V, int dtype, int w_layout, void* values_out, uint8_t* scales_out,
+                       int32_t* dev_status, void* stream) {
+    if (!W || !values_out || !scales_out) {
+        set_error("W, values_out and scales_out must not be NULL");
+        return RAPID_ERR_NULL;
+    }
+    int rc = validate_table("rapid_quantize_fp8", 1, 1, d, V, dtype, W, values_out);
+    if (rc) return rc;
+    if (w_layout != RAPID_W_DV && w_layout != RAPID_W_VD) {
+        set_error("unknown w_layout %d", w_layout);
+        return RAPID_ERR_DTYPE;
+    }
+    if ((uintptr_t)scales_out % 4 != 0) {
+        set_error("rapid_quantize_fp8: scales_out must be 4-byte aligned");
+        return RAPID_ERR_SHAPE;
+    }
+    rc = check_arch();
+    if (rc) return rc;
+    launch_quantize_fp8(W, V, d, dtype, w_layout, (uint8_t*)values_out, scales_out, dev_status, (hipStream_t)stream);
+    return check_launch("rapid_quantize_fp8");
+}
+
+int rapid_logprob_fwd_fp8(const void* hidden, const void* values, const uint8_t* scales, const int32_t* tokens, const uint8_t* mask,
+                          int64_t N, int64_t T, int64_t d, int64_t V, int dtype, float temperature, float* logp_out, float* lse_out,
+                          int32_t* dev_status, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!hidden || !values || !scales || !tokens || !mask || !logp_out) {
+        set_error("hidden, values, scales, tokens, mask and logp_out must not be NULL");
+        return RAPID_ERR_NULL;
+    }
+    int rc = validate_table("rapid_logprob_fwd_fp8", N, T, d, V, dtype, hidden, values);
+    if (rc) return rc;
+    if (!(temperature > 0.f) || !std::isfinite(temperature)) {
+        set_error("temperature must be finite and > 0");
+        return RAPID_ERR_SHAPE;
+    }
+    if ((uintptr_t)scales % 4 != 0) {
+        set_error("rapid_logprob_fwd_fp8: scales must be 4-byte aligned");
+        return RAPID_ERR_SHAPE;
+    }
+    Fp8Plan p;
+    if (!make_fp8_plan(p, N, T, d, V)) {
+        set_error("rapid_logprob_fwd_fp8: more than 2^25 positions (N=%lld T=%lld)", (long long)N, (long long)T);
+        return RAPID_ERR_SHAPE;
+    }
+    rc = validate_workspace("rapid_logprob_fwd_fp8", workspace, workspace_bytes, p.total);
+    if (!rc) rc = check_arch();
+    if (rc) return rc;
+    hipStream_t st = (hipStream_t)stream;
+    int32_t* counts = at<int32_t>(workspace, p.counts);
+    RowsArgs r;
+    r.mask = mask; r.N = N; r.T = T; r.region = INT64_MAX / 4; r.entries = 1; r.limits = counts;
+    r.row_index = at<int32_t>(workspace, p.row_index);
+    r.tokens = tokens; r.V = V; r.tokc = at<int32_t>(workspace, p.tokc); r.seqc = at<int32_t>(workspace, p.seqc);
+    r.dev_status = dev_status; r.zero_a = logp_out; r.zero_b = lse_out;
+    r.hidden = (const bf16_t*)hidden; r.hidden_f32 = dtype == RAPID_DTYPE_F32; r.d = d;
+    r.H8 = at<uint8_t>(workspace, p.H8); r.ld8 = p.ld8; r.h_scales = at<uint8_t>(workspace, p.h_scales);
+    r.W8 = (const uint8_t*)values; r.w_scales = scales;
+    r.inv_temp = 1.0f / temperature;
+    r.zy = at<float>(workspace, p.zy);
+    if (N * T <= ROWS_WITHOUT_PLAN && T <= BY_POSITION_T) {
+        r.counts_out = counts;
+    } else {
+        PlanArgs plan;
+        plan.N = N; plan.seq_len = at<int32_t>(workspace, p.seq_len); plan.cu = at<int32_t>(workspace, p.cu); plan.counts = counts;
+        launch_plan(mask, N, T, plan, st);
+        r.first_row = plan.cu;
+    }
+    launch_compact_rows(r, p.Mpad, st);
+    Fp8FwdArgs a;
+    a.W8 = r.W8; a.w_scales = r.w_scales; a.H8 = r.H8; a.h_scales = r.h_scales; a.V = V; a.d = d; a.ld8 = p.ld8;
+    a.tilesV = p.tilesV; a.inv_temp = r.inv_temp; a.counts = counts;
+    a.part_max = at<float>(workspace, p.part_max); a.part_sum = at<float>(workspace, p.part_sum); a.ld_part = p.Mpad;
+    a.gi = g_gi_fwd;
+    const int64_t block_rows = (int64_t)g_fwd_block_tiles.load() * 256;
+    for (int64_t r0 = 0; r0 < p.Mpad; r0 += block_rows) {
+        a.row0 = r0;
+        a.tilesM = (int)((p.Mpad - r0 < block_rows ? p.Mpad - r0 : block_rows) / 256);
+        launch_fwd_fp8(a, st);
+    }
+    launch_merge_lse(a.part_max, a.part_sum, p.tilesV * fwd_slots_per_tile(), p.Mpad, r.zy, r.row_index, counts, 0, p.Mpad,
+                     at<float>(workspace, p.lse_c), logp_out, lse_out, st, true);
+    return check_launch("rapid_logprob_fwd_fp8");
 }
 
 int rapid_group_advantage(const float* rewards, const int32_t* group_ids, const float* seq_logratio, int64_t N,

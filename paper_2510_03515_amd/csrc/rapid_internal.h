@@ -109,6 +109,12 @@ struct RowsArgs {
     float inv_temp = 1.f;
     float *zy = nullptr, *refz = nullptr;
     const float* ref_logp = nullptr;            // [N, T]
+    // 8-bit rows instead of packed ones (fp8.h; H8 set): `hidden` is then fp32 if hidden_f32, and W8 / w_scales are the head's
+    bool hidden_f32 = false;
+    uint8_t* H8 = nullptr;
+    int64_t ld8 = 0;                            // bytes
+    uint8_t* h_scales = nullptr;
+    const uint8_t *W8 = nullptr, *w_scales = nullptr;
 };
 // Positions up to which the rows may do without a plan (first_row NULL): every wave then counts the batch's mask up to its place.
 // Log-probs at d = 1024, V = 256 without a plan and with one: 64 x 32 positions 35 and 38 us, 64 x 64 42 and 45, 64 x 128 57 and 60;
@@ -124,10 +130,10 @@ void launch_compact_rows(const RowsArgs& a, int64_t rows, hipStream_t st);
 void launch_rows(const RowsArgs& a, bool by_position, int64_t rows, hipStream_t st);   // its part in rows.hip
 void launch_fill_f32(float* p, int64_t n, float v, hipStream_t st);
 // lse/logp from per-slot partial (max, sumexp) and the gathered logit, compact rows [row0, row0 + rows_max);
-// the partials of row j sit at column j - row0
+// the partials of row j sit at column j - row0.  cap: log-probs end at 0 (a gathered logit that was summed another way may be the larger one)
 void launch_merge_lse(const float* part_max, const float* part_sum, int P, int64_t ld_part,
                       const float* zy, const int32_t* row_index, const int32_t* counts, int64_t row0,
-                      int64_t rows_max, float* lse_c, float* logp_out, float* lse_out, hipStream_t st);
+                      int64_t rows_max, float* lse_c, float* logp_out, float* lse_out, hipStream_t st, bool cap = false);
 // The estimator kernels take `gen_range` (device, two words: first generation and one past the last; NULL =
 // all N): they then touch only those generations.
 // tsum/tmax (NULL or [N]): per generation, sum and log-maximum of its tokens' (clipped if clip_tokens) ratios
@@ -360,11 +366,48 @@ void set_waves_per_workgroup(int n);   // 4, 8 or 16 waves per contraction workg
 bool default_waves();                  // each kernel runs its own choice
 void set_dw_deep(int on);              // dW with K steps of 32 rows and requests three steps ahead
 void set_cu_count(int n);              // compute units of the device: the contraction kernels launch one workgroup each
+int cu_count();
 
 
 void launch_sgd_step(float* master, const float* grad, int64_t n, float lr, void* w_out, int dtype, hipStream_t st);
 void launch_adamw_step(float* master, const float* grad, float* m, float* v, int64_t n, float lr, float beta1, float beta2,
                        float eps, float weight_decay, int64_t step, void* w_out, int dtype, hipStream_t st);
+
+// ---- quantize.hip, gemm_fp8.hip ---------------------------------------------------------------
+void launch_quantize_fp8(const void* W, int64_t V, int64_t d, int dtype, int w_layout, uint8_t* values, uint8_t* scales, int32_t* dev_status, hipStream_t st);
+struct Fp8FwdArgs {       // 8-bit logits tile -> per-slot (max, sumexp), as FwdArgs
+    const uint8_t *W8, *w_scales;     // [V, fp8_row], [V, fp8_scale_row]: the caller's
+    const uint8_t *H8, *h_scales;     // [rows, ld8], [rows, fp8_scale_row], packed
+    int64_t V, d, ld8;
+    int tilesV, tilesM;               // 256-tiles; tilesM: of this launch, from row0 on
+    int64_t row0;
+    float inv_temp;
+    const int32_t* counts;
+    float *part_max, *part_sum;       // [2 tilesV][ld_part]
+    int64_t ld_part;
+    int gi;                           // tiles of the vocabulary that share one row tile before the order moves on
+};
+void launch_fwd_fp8(const Fp8FwdArgs& a, hipStream_t st);
+
+// ---- embedding.hip ------------------------------------------------------------------------------
+struct EmbeddingArgs {
+    const int32_t* tokens = nullptr;   // [positions]
+    const uint8_t* mask = nullptr;     // [positions] or NULL: all valid
+    int64_t positions = 0, d = 0, V = 0;
+    int dtype = 0;                     // of the table and of the hidden states
+    float scale = 1.f;
+    int32_t* dev_status = nullptr;
+};
+void launch_embedding_fwd(const EmbeddingArgs& a, const void* table, void* out, hipStream_t st);
+// how the backward sorts and shares out a batch of so many positions, and where its scratch lies
+struct EmbeddingPlan {
+    int passes, bits;                  // radix passes and bits of the id in each
+    int64_t tile, blocks;              // positions per block of a pass
+    int64_t rows, stretches;           // sorted positions that a group of threads adds up
+    size_t counts, key[2], pos[2], hist, touched, part, total;
+};
+EmbeddingPlan embedding_plan(int64_t positions, int64_t d, int64_t V);
+void launch_embedding_bwd(const EmbeddingArgs& a, const EmbeddingPlan& p, void* ws, const void* dh, int dw_dtype, int accumulate, void* dE, hipStream_t st);
 
 // ---- probe.hip -----------------------------------------------------------------------------------
 int run_mfma_probe(int random_operands, int iters, int num_cu, double* tflops_out, double* ms_out, hipStream_t st);

@@ -505,7 +505,7 @@ __global__ __launch_bounds__(64 * NW) void merge_lse_kernel(const float* __restr
                                  int64_t ld_part, const float* __restrict__ zy,
                                  const int32_t* __restrict__ row_index, const int32_t* __restrict__ counts,
                                  int64_t row0, float* __restrict__ lse_c, float* __restrict__ logp_out,
-                                 float* __restrict__ lse_out) {
+                                 float* __restrict__ lse_out, bool cap) {
     constexpr int GROUPS = 2 * NW;
     __shared__ float s_mx[NW][32];
     __shared__ double s_acc[NW][32];
@@ -544,7 +544,8 @@ __global__ __launch_bounds__(64 * NW) void merge_lse_kernel(const float* __restr
     const float lse_f = (float)lse;
     lse_c[j] = lse_f;
     const int32_t pos = row_index[j];
-    logp_out[pos] = (float)((double)zy[j] - lse);
+    const float logp = (float)((double)zy[j] - lse);
+    logp_out[pos] = cap && logp > 0.f ? 0.f : logp;
     if (lse_out) lse_out[pos] = lse_f;
 }
 
@@ -555,7 +556,7 @@ __global__ __launch_bounds__(256) void merge_lse_few_kernel(const float* __restr
                                  int64_t ld_part, const float* __restrict__ zy,
                                  const int32_t* __restrict__ row_index, const int32_t* __restrict__ counts,
                                  int64_t row0, float* __restrict__ lse_c, float* __restrict__ logp_out,
-                                 float* __restrict__ lse_out) {
+                                 float* __restrict__ lse_out, bool cap) {
     constexpr int GROUPS = 32, COLS = 8;
     __shared__ float s_mx[GROUPS][COLS];
     __shared__ double s_acc[GROUPS][COLS];
@@ -585,7 +586,8 @@ __global__ __launch_bounds__(256) void merge_lse_few_kernel(const float* __restr
     const float lse_f = (float)lse;
     lse_c[j] = lse_f;
     const int32_t pos = row_index[j];
-    logp_out[pos] = (float)((double)zy[j] - lse);
+    const float logp = (float)((double)zy[j] - lse);
+    logp_out[pos] = cap && logp > 0.f ? 0.f : logp;
     if (lse_out) lse_out[pos] = lse_f;
 }
 
@@ -1193,7 +1195,7 @@ void launch_compact_rows(const RowsArgs& a, int64_t rows, hipStream_t st) {
     const unsigned threads = row_threads(a.T);
     (threads == WAVE ? &row_index_kernel<true> : &row_index_kernel<false>)<<<(unsigned)a.N, threads, 0, st>>>(a);
     if (a.dhidden) zero_masked_rows_kernel<<<(unsigned)(a.N * a.T), 128, 0, st>>>(a.dhidden, a.mask, a.N * a.T, a.words_per_row, a.idle, a.T);
-    if (a.Hc) launch_rows(a, false, rows, st);
+    if (a.Hc || a.H8) launch_rows(a, false, rows, st);
 }
 
 void launch_fill_f32(float* p, int64_t n, float v, hipStream_t st) {
@@ -1205,15 +1207,15 @@ void launch_f32_add(const float* src, float* dst, int64_t n, hipStream_t st) {
 
 void launch_merge_lse(const float* part_max, const float* part_sum, int P, int64_t ld_part, const float* zy,
                       const int32_t* row_index, const int32_t* counts, int64_t row0, int64_t rows_max, float* lse_c,
-                      float* logp_out, float* lse_out, hipStream_t st) {
+                      float* logp_out, float* lse_out, hipStream_t st, bool cap) {
     if (rows_max <= 0) return;
     if (P > 128 && rows_max <= 1024) {
-        merge_lse_few_kernel<<<blocks_for(rows_max, 8), 256, 0, st>>>(part_max, part_sum, P, ld_part, zy, row_index, counts, row0, lse_c, logp_out, lse_out);
+        merge_lse_few_kernel<<<blocks_for(rows_max, 8), 256, 0, st>>>(part_max, part_sum, P, ld_part, zy, row_index, counts, row0, lse_c, logp_out, lse_out, cap);
         return;
     }
     auto* kernel = P <= 16 ? &merge_lse_kernel<1> : P <= 128 ? &merge_lse_kernel<4> : &merge_lse_kernel<16>;
     kernel<<<blocks_for(rows_max, 32), P <= 16 ? 64 : P <= 128 ? 256 : 1024, 0, st>>>(part_max, part_sum, P, ld_part, zy, row_index,
-                                                                                     counts, row0, lse_c, logp_out, lse_out);
+                                                                                     counts, row0, lse_c, logp_out, lse_out, cap);
 }
 
 void launch_seq_logratio(const float* logp_cur, const float* logp_behav, const uint8_t* mask, int64_t N,

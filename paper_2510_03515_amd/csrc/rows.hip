@@ -10,13 +10,14 @@
 // of the batch; where that does not pay (launch_compact_rows) the rows are indexed by row_index_kernel first and the waves here
 // take compact rows.
 #include "rapid_internal.h"
+#include "fp8.h"
 #include "row_math.h"
 
 namespace rapid {
 
 namespace {
 
-enum { PACK_NONE = 0, PACK_COPY, PACK_RMS };
+enum { PACK_NONE = 0, PACK_COPY, PACK_RMS, PACK_FP8_BF16, PACK_FP8_F32 };
 constexpr int U = 4;     // 16-byte chunks per lane whose loads are in flight together
 
 __device__ inline void zero_row(void* p, int64_t words) {
@@ -129,13 +130,66 @@ __device__ __forceinline__ void pack_row(const RowsArgs& a, int64_t j, int64_t p
     }
 }
 
+// The same with 8-bit rows (fp8.h): H8[j] = hidden row `pos` in blocks of 128 with their scales, and zy[j] the product of what was stored with the
+// token's 8-bit weights, summed in fp32 (a block's sum takes its scale at once; then a fixed tree over the lanes).
+template <class T>
+__device__ __forceinline__ void pack_row_fp8(const RowsArgs& a, int64_t j, int64_t pos, int token) {
+    const int lane = threadIdx.x & 63;
+    const int64_t bytes = fp8_row(a.d), scale_row = fp8_scale_row(a.d);
+    const T* src = (const T*)a.hidden + pos * a.d;
+    uint8_t* dst = a.H8 + j * a.ld8;
+    const uint8_t* w = a.W8 + (int64_t)token * bytes;
+    const uint8_t* ws = a.w_scales + (int64_t)token * scale_row;
+    float acc = 0.f;
+    bool bad = false;
+    for (int64_t base = 0; base < bytes; base += 512) {
+        const int64_t c = base + lane * 8;
+        float x[8], h[4], g[4];
+        load8(src, c, a.d, x);
+        uint2 wv = make_uint2(0u, 0u);
+        uint32_t w_scale = 127u, s;
+        if (c < bytes) {
+            wv = *(const uint2*)(w + c);
+            w_scale = ws[c / FP8_BLOCK];
+        }
+        const uint2 q = quantize_block(x, s, bad);
+        if (c < bytes) *(uint2*)(dst + c) = q;
+        float part = 0.f;
+        from_fp8x4(q.x, h); from_fp8x4(wv.x, g);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) part = fmaf(h[e], g[e], part);
+        from_fp8x4(q.y, h); from_fp8x4(wv.y, g);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) part = fmaf(h[e], g[e], part);
+        acc = fmaf(part * scale_value(s), scale_value(w_scale), acc);
+        const uint32_t word = scale_word(s);
+        if (lane == 0) *(uint32_t*)(a.h_scales + j * scale_row + base / FP8_BLOCK) = word;
+    }
+    if (bad && a.dev_status) atomicOr(a.dev_status, RAPID_STATUS_NONFINITE_VALUE);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) acc += __shfl_xor(acc, o, 64);
+    if (lane == 0) a.zy[j] = acc * a.inv_temp;
+}
+
+template <int PACK, bool GATHER>
+__device__ __forceinline__ void pack_any(const RowsArgs& a, int64_t j, int64_t pos, int token) {
+    if constexpr (PACK == PACK_FP8_BF16) pack_row_fp8<bf16_t>(a, j, pos, token);
+    else if constexpr (PACK == PACK_FP8_F32) pack_row_fp8<float>(a, j, pos, token);
+    else pack_row<PACK, GATHER>(a, j, pos, token);
+}
+
 // rows that fill a region's last row tile up: token 0, zeros
-__device__ __forceinline__ void fill_row(const RowsArgs& a, int64_t j, bool pack) {
+template <int PACK>
+__device__ __forceinline__ void fill_row(const RowsArgs& a, int64_t j) {
     if ((threadIdx.x & 63) == 0 && a.tokc) {
         a.tokc[j] = 0;
         a.seqc[j] = 0;
     }
-    if (pack) zero_row(a.Hc + j * a.ldk, a.Cpad / 2);
+    if constexpr (PACK == PACK_COPY || PACK == PACK_RMS) zero_row(a.Hc + j * a.ldk, a.Cpad / 2);
+    if constexpr (PACK == PACK_FP8_BF16 || PACK == PACK_FP8_F32) {
+        zero_row(a.H8 + j * a.ld8, fp8_row(a.d) / 4);
+        zero_row(a.h_scales + j * fp8_scale_row(a.d), fp8_scale_row(a.d) / 4);
+    }
 }
 
 // the wave's valid positions among the first n of `mask`: 16-byte words, and one lane each for the bytes in front of the first
@@ -181,7 +235,7 @@ __global__ __launch_bounds__(256) void rows_by_position_kernel(RowsArgs a, int p
                 a.counts_out[CNT_MR] = (int32_t)end;
             }
         }
-        for (int64_t j = M + part * waves + wave; j < end; j += 16 * waves) fill_row(a, j, PACK != PACK_NONE);
+        for (int64_t j = M + part * waves + wave; j < end; j += 16 * waves) fill_row<PACK>(a, j);
         return;
     }
     const int64_t n = b / blocks_per_generation;
@@ -215,7 +269,7 @@ __global__ __launch_bounds__(256) void rows_by_position_kernel(RowsArgs a, int p
     const unsigned long long rows = __ballot(placed);
     for (int i = 0; i < per_wave && t0 + i < T; ++i) {
         if constexpr (PACK != PACK_NONE) {
-            if ((rows >> i) & 1ull) pack_row<PACK, GATHER>(a, __shfl(j_mine, i, 64), n * T + t0 + i, __shfl(tok, i, 64));
+            if ((rows >> i) & 1ull) pack_any<PACK, GATHER>(a, __shfl(j_mine, i, 64), n * T + t0 + i, __shfl(tok, i, 64));
         }
         if (a.dhidden && (idle || !((votes >> i) & 1ull))) zero_row(a.dhidden + (n * T + t0 + i) * a.words_per_row, a.words_per_row);
     }
@@ -227,8 +281,8 @@ __global__ __launch_bounds__(256) void rows_by_row_kernel(RowsArgs a) {
     const int64_t j = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
     const int32_t* lim = a.limits + j / a.region * a.stride;
     if (j >= lim[CNT_MR]) return;
-    if (j < lim[CNT_M]) pack_row<PACK, GATHER>(a, j, a.row_index[j], a.tokc[j]);
-    else fill_row(a, j, true);
+    if (j < lim[CNT_M]) pack_any<PACK, GATHER>(a, j, a.row_index[j], a.tokc[j]);
+    else fill_row<PACK>(a, j);
 }
 
 template <int PACK, bool GATHER>
@@ -250,7 +304,8 @@ void launch_t(const RowsArgs& a, bool by_position, int64_t rows, hipStream_t st)
 }  // namespace
 
 void launch_rows(const RowsArgs& a, bool by_position, int64_t rows, hipStream_t st) {
-    if (!a.Hc) launch_t<PACK_NONE, false>(a, by_position, rows, st);
+    if (a.H8) a.hidden_f32 ? launch_t<PACK_FP8_F32, false>(a, by_position, rows, st) : launch_t<PACK_FP8_BF16, false>(a, by_position, rows, st);
+    else if (!a.Hc) launch_t<PACK_NONE, false>(a, by_position, rows, st);
     else if (a.rms_weight) a.gather ? launch_t<PACK_RMS, true>(a, by_position, rows, st) : launch_t<PACK_RMS, false>(a, by_position, rows, st);
     else a.gather ? launch_t<PACK_COPY, true>(a, by_position, rows, st) : launch_t<PACK_COPY, false>(a, by_position, rows, st);
 }
