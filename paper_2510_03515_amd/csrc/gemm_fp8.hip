@@ -442,22 +442,214 @@ __global__ __launch_bounds__(S::NT, 1) void fwd_fp8_kernel(Fp8FwdArgs a) {
     }
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
-template <class S>
-void launch_t(const Fp8FwdArgs& a, hipStream_t st) {
-    const int ids = ids_for(a.tilesV, a.tilesM * (256 / S::BJ)), cus = cu_count() / 8 * 8;
-    const unsigned grid = (unsigned)(ids < cus ? ids : cus);
-    constexpr int stages = 2 * (S::BI + S::BJ) * 128, scales = 2 * (S::BI + S::BJ) * 4;
-    if (a.V >= S::BI && a.d > FP8_BLOCK) {
-        allow_lds<&fwd_fp8_kernel<S>>(stages + scales);
-        fwd_fp8_kernel<S><<<grid, S::NT, stages + scales, st>>>(a);
-    } else {
-        allow_lds<&fwd_fp8_small_kernel<S>>(stages);
-        fwd_fp8_small_kernel<S><<<grid, S::NT, stages, st>>>(a);
+// Running maximum m (of the logits before the temperature) and sum l of every row over a wave's 32 columns of another tile, of which the first `seen`
+// belong to the tile before.
+template <int WJ>
+__device__ __forceinline__ void add_tile(f32x16 (&acc)[WJ], int seen, int hi4, float zs, float (&m)[WJ], float (&l)[WJ]) {
+#pragma unroll
+    for (int jb = 0; jb < WJ; ++jb) {
+        float mx = m[jb];
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            if ((v >> 2) * 8 + hi4 + (v & 3) < seen) acc[jb][v] = -INFINITY;
+            mx = fmaxf(mx, acc[jb][v]);
+        }
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        const float nm = mx == -INFINITY ? 0.f : -mx * zs;
+        float sum = l[jb] * __builtin_amdgcn_exp2f(m[jb] == -INFINITY ? -INFINITY : fmaf(m[jb], zs, nm));
+#pragma unroll
+        for (int v = 0; v < 16; ++v) sum += __builtin_amdgcn_exp2f(fmaf(acc[jb][v], zs, nm));
+        m[jb] = mx;
+        l[jb] = sum;
     }
+}
+// The workgroup's slot: the sums of a lane pair, then of the four waves that share rows from row0 on (wave: 0 .. 3 among them), in order.  `shared` has
+// 256 WJ floats for them; a NaN becomes +infinity (see epilogue_rows).
+template <int WJ>
+__device__ __forceinline__ void leave_slot(const Fp8FwdArgs& a, float* shared, int wave, int row0, float zs, float (&m)[WJ], float (&l)[WJ]) {
+    const int lane = threadIdx.x & 63;
+    __syncthreads();                    // nobody reads the stages any more
+#pragma unroll
+    for (int jb = 0; jb < WJ; ++jb) {
+        l[jb] += __shfl_xor(l[jb], 32, 64);
+        if (lane < 32) {
+            shared[(wave * WJ + jb) * 64 + lane] = m[jb];
+            shared[(wave * WJ + jb) * 64 + 32 + lane] = l[jb];
+        }
+    }
+    __syncthreads();
+    if (wave != 0 || lane >= 32) return;
+#pragma unroll
+    for (int jb = 0; jb < WJ; ++jb) {
+        float mx = m[jb], sum = 0.f;
+#pragma unroll
+        for (int w = 1; w < 4; ++w) mx = fmaxf(mx, shared[(w * WJ + jb) * 64 + lane]);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float mw = shared[(w * WJ + jb) * 64 + lane], lw = shared[(w * WJ + jb) * 64 + 32 + lane];
+            sum += lw == 0.f ? 0.f : lw * __builtin_amdgcn_exp2f((mw - mx) * zs);
+        }
+        if (sum != sum) { mx = INFINITY; sum = 1.f; }
+        a.part_max[(int64_t)blockIdx.x * a.ld_part + row0 + jb * 32 + lane] = mx * a.inv_temp;
+        a.part_sum[(int64_t)blockIdx.x * a.ld_part + row0 + jb * 32 + lane] = sum;
+    }
+}
+
+// Few rows (at most 32 WJ, all of them in every tile): the head is read once for next to no products, so what counts is that its bytes never stop coming.
+// A workgroup of 4 waves takes tiles of 128 vocabulary rows (a wave 32 of them) through a ring of NST stages, requests NST - 1 steps ahead across the ends of
+// tiles (16 KB of the head in each: 128 KB of them on their way per CU hide a trip to HBM at full rate).  Every step asks for the
+// word of scales that it lies in, so that all steps make the same requests and one count of outstanding ones fits all.  The sums over the
+// vocabulary run on in registers from tile to tile; a workgroup leaves one slot.
+template <int WJ_, int NST_>
+struct Few {
+    static constexpr int WJ = WJ_, NST = NST_, BI = 128, BJ = 32 * WJ, ROWS = BI + BJ, NW = 4;
+    static constexpr int STAGE = ROWS * 128, SCB = 256 * 4, LDS = NST * (STAGE + SCB);
+    static constexpr int NA = BI / (8 * NW), NB = BJ / (8 * NW), T = NA + NB + 1;      // requests of a wave and step
+};
+template <class F>
+__global__ __launch_bounds__(64 * F::NW, 1) void fwd_fp8_few_kernel(Fp8FwdArgs a) {
+    constexpr int WJ = F::WJ, NST = F::NST, BI = F::BI, D = NST - 1;
+    extern __shared__ __attribute__((aligned(128))) char lds[];
+    if (a.counts[CNT_MR] == 0) return;
+    const int64_t row = fp8_row(a.d), scale_row = fp8_scale_row(a.d);
+    const int steps = (int)(row / FP8_BLOCK), tiles = (int)((a.V + BI - 1) / BI);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    // workgroups of an XCD take neighbouring tiles; the last tile begins where it ends with the vocabulary
+    const int wgs = gridDim.x, mine = (blockIdx.x & 7) * (wgs / 8) + (blockIdx.x >> 3);
+    auto first_v = [&](int ti) { return (int)min((int64_t)ti * BI, a.V - BI); };
+    const int chunk = (lane & 7) ^ ((((wave & 1) << 2) + (lane >> 4)) & 7);
+    const uint32_t off_a = (uint32_t)((lane >> 3) * row + chunk * 16), off_b = (uint32_t)((lane >> 3) * a.ld8 + chunk * 16);
+    const char* const hidden = (const char*)a.H8 + (int64_t)(wave * 8) * a.ld8;
+    // scales: a wave's request covers rows 64 wave .. + 63 of the tile's (rows that are none of it repeat its last one)
+    const int srow = min(64 * wave + lane, F::ROWS - 1);
+    const uint32_t off_s = (uint32_t)((srow < BI ? srow : srow - BI) * (int)scale_row);
+    const bool of_head = 64 * wave < BI;
+
+    int tq = mine, kq = 0, sq = 0;      // the next requests: tile, step, stage
+    const char* ga = (const char*)a.W8 + (first_v(tq) + wave * 8) * row;
+    auto ask = [&]() {
+        char* to = lds + sq * F::STAGE + wave * 1024;
+        const auto ra = __builtin_amdgcn_make_buffer_rsrc((void*)ga, 0, -1, 0x00020000), rb = __builtin_amdgcn_make_buffer_rsrc((void*)hidden, 0, -1, 0x00020000);
+#pragma unroll
+        for (int r = 0; r < F::NA; ++r)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (__attribute__((address_space(3))) void*)(to + r * 4096), 16, off_a, r * 32 * (int)row + kq * 128, 0, 0);
+#pragma unroll
+        for (int r = 0; r < F::NB; ++r)
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(rb, (__attribute__((address_space(3))) void*)(to + BI * 128 + r * 4096), 16, off_b,
+                                                     r * 32 * (int)a.ld8 + kq * 128, 0, 0);
+        const uint8_t* base = of_head ? a.w_scales + first_v(tq) * scale_row : a.h_scales;
+        load_to_lds_4((const char*)base + (kq & ~3) + off_s, lds + NST * F::STAGE + sq * F::SCB + wave * 256);
+        sq = sq == NST - 1 ? 0 : sq + 1;
+        if (++kq == steps) {
+            if (tq + wgs < tiles) {
+                kq = 0;
+                tq += wgs;
+                ga = (const char*)a.W8 + (first_v(tq) + wave * 8) * row;
+            } else {
+                kq = steps - 1;         // none is left: the last step again, into stages that nobody reads
+            }
+        }
+    };
+    const uint32_t in_row = (lane & 31) * 128 + (((lane >> 5) ^ ((lane >> 1) & 7)) * 16);
+    const uint32_t at_a = lds_addr(lds) + wave * 4096 + in_row, at_b = lds_addr(lds) + BI * 128 + in_row;
+    const uint32_t at_s = lds_addr(lds) + NST * F::STAGE + (lane & 31) * 4;
+    const float zs = a.inv_temp * LOG2E;
+    const int hi4 = (lane >> 5) * 4;
+    float m[WJ], l[WJ];                 // running maximum (of the logits before the temperature) and sum of every row
+#pragma unroll
+    for (int jb = 0; jb < WJ; ++jb) { m[jb] = -INFINITY; l[jb] = 0.f; }
+    if (mine < tiles) {
+#pragma unroll
+        for (int s = 0; s < D; ++s) ask();
+        int cur = 0;
+        for (int ti = mine; ti < tiles; ti += wgs) {
+            f32x16 acc[1][WJ];
+#pragma unroll
+            for (int jb = 0; jb < WJ; ++jb)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) acc[0][jb][v] = 0.f;
+            for (int kt = 0; kt < steps; ++kt) {
+                asm volatile("s_waitcnt vmcnt(%0)" ::"n"((D - 1) * F::T) : "memory");      // the step has landed
+                lds_barrier();                                                             // everybody's; the stage before this one is free
+                ask();
+                const uint32_t stage = cur * F::STAGE, byte = cur * F::SCB + (kt & 3);
+                Bytes<1> sa;
+                Bytes<WJ> sb;
+                read_bytes(sa, at_s + wave * 128 + byte);
+                read_bytes(sb, at_s + BI * 4 + byte);
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    Frag<1> fa;
+                    Frag<WJ> fb;
+                    read_frag(fa, at_a + stage, s);
+                    read_frag(fb, at_b + stage, s);
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                    Whole<1> wa;
+                    Whole<WJ> wb;
+                    take(wa, fa);
+                    take(wb, fb);
+                    arrived(sa);
+                    arrived(sb);
+#pragma unroll
+                    for (int jb = 0; jb < WJ; ++jb)
+                        acc[0][jb] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wa.v[0], wb.v[jb], acc[0][jb], 0, 0, 0, (int)sa.v[0], 0, (int)sb.v[jb]);
+                }
+                cur = cur == NST - 1 ? 0 : cur + 1;
+            }
+            add_tile<WJ>(acc[0], ti * BI - first_v(ti) - wave * 32, hi4, zs, m, l);
+        }
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    leave_slot<WJ>(a, (float*)lds, wave, 0, zs, m, l);
+}
+
+template <class S>
+unsigned tile_grid(const Fp8FwdArgs& a) {
+    const int ids = ids_for(a.tilesV, a.tilesM * (256 / S::BJ)), cus = cu_count() / 8 * 8;
+    return (unsigned)(ids < cus ? ids : cus);
+}
+template <class S>
+void launch_small(const Fp8FwdArgs& a, hipStream_t st) {
+    constexpr int stages = 2 * (S::BI + S::BJ) * 128;
+    allow_lds<&fwd_fp8_small_kernel<S>>(stages);
+    fwd_fp8_small_kernel<S><<<tile_grid<S>(a), S::NT, stages, st>>>(a);
+}
+template <class S>
+void launch_tiles(const Fp8FwdArgs& a, hipStream_t st) {
+    constexpr int bytes = 2 * (S::BI + S::BJ) * (128 + 4);
+    allow_lds<&fwd_fp8_kernel<S>>(bytes);
+    fwd_fp8_kernel<S><<<tile_grid<S>(a), S::NT, bytes, st>>>(a);
+}
+template <class F>
+void launch_few(const Fp8FwdArgs& a, int slots, hipStream_t st) {
+    allow_lds<&fwd_fp8_few_kernel<F>>(F::LDS);
+    fwd_fp8_few_kernel<F><<<(unsigned)slots, 64 * F::NW, F::LDS, st>>>(a);
+}
+typedef Geo<2, 4, 4, 2> Tiles;
+
+// slots of the kernels that stream the head past all rows: one per workgroup, a multiple of 8 of them
+int stream_slots(int64_t V) {
+    const int cus = cu_count() / 8 * 8, wanted = (int)((V + 127) / 128 + 7) / 8 * 8;
+    return wanted < cus ? wanted : cus;
 }
 
 }  // namespace
 
-void launch_fwd_fp8(const Fp8FwdArgs& a, hipStream_t st) { launch_t<Geo<2, 4, 4, 2>>(a, st); }
+// 16 rows, d 1536, V 151936: tiles 65 us, the head read at 3.6 TB/s; few rows 36.7 us, 6.4 TB/s.  60 rows: 65 and 38.6 us.
+Fp8Way fp8_way(int64_t positions, int64_t d, int64_t V) {
+    if (V >= Tiles::BI && d > FP8_BLOCK && positions <= 64) return Fp8Way{positions <= 32 ? FP8_32_ROWS : FP8_64_ROWS, stream_slots(V)};
+    return Fp8Way{V >= Tiles::BI && d > FP8_BLOCK ? FP8_TILES : FP8_SMALL_HEAD, 2 * (int)((V + 255) / 256)};
+}
+
+int64_t fp8_most_slots(int64_t V) { return 2 * ((V + 255) / 256) + 8; }     // two a tile; or one per 128 entries, up to a multiple of 8
+
+void launch_fwd_fp8(const Fp8FwdArgs& a, const Fp8Way& p, hipStream_t st) {
+    switch (p.kernel) {
+    case FP8_SMALL_HEAD: launch_small<Tiles>(a, st); break;
+    case FP8_32_ROWS: launch_few<Few<1, 7>>(a, p.slots, st); break;
+    case FP8_64_ROWS: launch_few<Few<2, 6>>(a, p.slots, st); break;
+    case FP8_TILES: launch_tiles<Tiles>(a, st); break;
+    }
+}
 
 }  // namespace rapid

@@ -682,8 +682,9 @@ bool make_fp8_plan(Fp8Plan& p, int64_t N, int64_t T, int64_t d, int64_t V) {
     p.lse_c = take(cur, (size_t)p.Mpad * 4);
     p.h_scales = take(cur, (size_t)p.Mpad * fp8_scale_row(d));
     p.H8 = take(cur, (size_t)p.Mpad * p.ld8);
-    p.part_max = take(cur, (size_t)p.tilesV * fwd_slots_per_tile() * p.Mpad * 4);
-    p.part_sum = take(cur, (size_t)p.tilesV * fwd_slots_per_tile() * p.Mpad * 4);
+    const size_t slots = (size_t)fp8_most_slots(V);
+    p.part_max = take(cur, slots * p.Mpad * 4);
+    p.part_sum = take(cur, slots * p.Mpad * 4);
     p.total = cur;
     return true;
 }
@@ -1147,13 +1148,14 @@ int rapid_logprob_fwd_fp8(const void* hidden, const void* values, const uint8_t*
     a.tilesV = p.tilesV; a.inv_temp = r.inv_temp; a.counts = counts;
     a.part_max = at<float>(workspace, p.part_max); a.part_sum = at<float>(workspace, p.part_sum); a.ld_part = p.Mpad;
     a.gi = g_gi_fwd;
+    const Fp8Way way = fp8_way(N * T, d, V);
     const int64_t block_rows = (int64_t)g_fwd_block_tiles.load() * 256;
     for (int64_t r0 = 0; r0 < p.Mpad; r0 += block_rows) {
         a.row0 = r0;
         a.tilesM = (int)((p.Mpad - r0 < block_rows ? p.Mpad - r0 : block_rows) / 256);
-        launch_fwd_fp8(a, st);
+        launch_fwd_fp8(a, way, st);
     }
-    launch_merge_lse(a.part_max, a.part_sum, p.tilesV * fwd_slots_per_tile(), p.Mpad, r.zy, r.row_index, counts, 0, p.Mpad,
+    launch_merge_lse(a.part_max, a.part_sum, way.slots, p.Mpad, r.zy, r.row_index, counts, 0, p.Mpad,
                      at<float>(workspace, p.lse_c), logp_out, lse_out, st, true);
     return check_launch("rapid_logprob_fwd_fp8");
 }

@@ -387,7 +387,12 @@ struct Fp8FwdArgs {       // 8-bit logits tile -> per-slot (max, sumexp), as Fwd
     int64_t ld_part;
     int gi;                           // tiles of the vocabulary that share one row tile before the order moves on
 };
-void launch_fwd_fp8(const Fp8FwdArgs& a, hipStream_t st);
+// Kernels, by the call's sizes (few rows: the head streams past all of them at once), and the slots of partial sums that they leave per row
+enum Fp8Kernel { FP8_SMALL_HEAD, FP8_32_ROWS, FP8_64_ROWS, FP8_TILES };
+struct Fp8Way { Fp8Kernel kernel; int slots; };
+Fp8Way fp8_way(int64_t positions, int64_t d, int64_t V);
+int64_t fp8_most_slots(int64_t V);                 // of any of them
+void launch_fwd_fp8(const Fp8FwdArgs& a, const Fp8Way& way, hipStream_t st);
 
 // ---- embedding.hip ------------------------------------------------------------------------------
 struct EmbeddingArgs {
