@@ -370,7 +370,7 @@ int rapid_embedding_fwd(const void* table, const int32_t* tokens, const uint8_t*
  *   dtable_out[v,:] = scale * sum of dhidden[n,t,:] over the valid positions with tokens[n,t] = v     (accumulate = 0)
  *   dtable_out[v,:] += the same; rows of ids that do not occur are not touched                        (accumulate = 1)
  * dhidden in `dtype` (masked positions are not read), dtable_out in dw_dtype (accumulate: fp32 only), both 16-byte aligned.
- * Sums are fp32, in an order that depends on the positions of an id and on N * T alone: the same inputs give the same bits.
+ * Sums are fp32, in an order that depends on the valid positions and their ids alone: the same inputs give the same bits.
  * Workspace: rapid_workspace_bytes(RAPID_OP_EMBEDDING_BWD, N, T, d, V, ., dtype).
  */
 int rapid_embedding_bwd(const void* dhidden, const int32_t* tokens, const uint8_t* mask, int64_t N, int64_t T,

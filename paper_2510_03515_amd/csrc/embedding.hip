@@ -5,6 +5,7 @@
 //
 // Both are bound by memory.  The backward sorts the valid positions by (token, position) first, so that every row of dE is formed by one
 // owner, in one order that hangs on the batch's size alone: no floating-point atomics, the same bits in every run.
+#include "mfma_tiles.h"
 #include "rapid_internal.h"
 #include "row_math.h"
 
@@ -94,7 +95,7 @@ void fwd_t(const EmbeddingArgs& a, const void* table, void* out, hipStream_t st)
 // digit's bits give the lanes that share it, a wave-private count in the LDS the items of earlier rounds.
 // The first pass reads ids and mask in the order of the positions and drops what has no row.
 constexpr int MAX_DIGIT_BITS = 9, MAX_DIGITS = 1 << MAX_DIGIT_BITS;
-constexpr int SORT_WAVES = 8, SORT_THREADS = 64 * SORT_WAVES, SORT_ITEMS = 8;      // a round of a block: 4096 items
+constexpr int SORT_WAVES = 8, SORT_THREADS = 64 * SORT_WAVES;
 
 struct SortPass {
     const int32_t *tokens; const uint8_t* mask; int V; int32_t* dev_status;       // first pass
@@ -102,39 +103,99 @@ struct SortPass {
     int32_t *key_out, *pos_out;
     int32_t* hist;          // [blocks][digits]
     int32_t* counts;        // [0] = number of valid positions (written by the first pass's scatter)
-    uint32_t* touched;      // NULL, or one bit per id: set for the ids that occur (first pass, zero before)
-    int64_t items, tile;
+    uint32_t* flags;        // NULL, or flag_words words that the first pass clears
+    int64_t items, tile, flag_words;
     int shift, bits, blocks;
 };
 
-template <bool FIRST>
-__device__ __forceinline__ int sort_key(const SortPass& a, int64_t i, int64_t end, int32_t* status) {
-    if (i >= end) return -1;
-    return FIRST ? valid_token(a.tokens, a.mask, i, a.V, status) : a.key_in[i];
+// ids of U items, `step` apart from i on (-1: none, masked, or out of range): all loads first, a chain of one trip
+template <bool FIRST, int U>
+__device__ __forceinline__ void sort_keys(const SortPass& a, int64_t i, int64_t step, int64_t end, bool flag, int (&key)[U], int (&pos)[U]) {
+    uint8_t m[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int64_t at = i + u * step < end ? i + u * step : end - 1;
+        key[u] = FIRST ? a.tokens[at] : a.key_in[at];
+        pos[u] = FIRST ? (int)at : a.pos_in[at];
+        m[u] = FIRST && a.mask ? a.mask[at] : 1;
+    }
+    bool bad = false;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const bool here = i + u * step < end && m[u] != 0, in = !FIRST || (key[u] >= 0 && key[u] < a.V);
+        bad |= here && !in;
+        if (!here || !in) key[u] = -1;
+    }
+    if (FIRST && flag && bad && a.dev_status) atomicOr(a.dev_status, RAPID_STATUS_BAD_TOKEN);
+}
+__device__ __forceinline__ void clear_flags(const SortPass& a, int64_t i, int64_t step) {
+    if (a.flags)
+        for (; i < a.flag_words; i += step) a.flags[i] = 0u;
+}
+// lanes with the same digit as this one, among those with an item
+__device__ __forceinline__ unsigned long long same_digit(int digit, int bits, bool item) {
+    unsigned long long same = __ballot(item);
+    for (int b = 0; b < bits; ++b) {
+        const unsigned long long votes = __ballot((digit >> b) & 1);
+        same &= ((digit >> b) & 1) ? votes : ~votes;
+    }
+    return same;
+}
+// Ranks of a wave's items of one round among its items of the same digit.  count: the wave's own counters in the LDS (its lanes run in step).
+__device__ __forceinline__ int rank_in_wave(int key, int digit, int bits, int* count) {
+    const unsigned long long same = same_digit(digit, bits, key >= 0);
+    int rank = 0;
+    if (key >= 0) {
+        const int ahead = __popcll(same & ((1ull << (threadIdx.x & 63)) - 1ull)), old = count[digit];
+        rank = old + ahead;
+        __builtin_amdgcn_wave_barrier();
+        if (ahead == 0) count[digit] = old + __popcll(same);
+    }
+    __builtin_amdgcn_wave_barrier();
+    return rank;
+}
+// sums of v over the threads before this one and over all of them; s_sum [waves]
+template <int WAVES>
+__device__ __forceinline__ void scan_threads(int v, int* s_sum, int& before, int& all) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int run = v;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+        const int w = __shfl_up(run, o, 64);
+        if (lane >= o) run += w;
+    }
+    if (lane == 63) s_sum[wave] = run;
+    __syncthreads();
+    before = run - v;
+    all = 0;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+        if (w < wave) before += s_sum[w];
+        all += s_sum[w];
+    }
 }
 
-template <bool FIRST>
+template <bool FIRST, int SORT_ITEMS>
 __global__ __launch_bounds__(SORT_THREADS) void sort_count_kernel(SortPass a) {
     __shared__ int s_hist[MAX_DIGITS];
     const int digits = 1 << a.bits;
     for (int i = threadIdx.x; i < digits; i += SORT_THREADS) s_hist[i] = 0;
+    if (FIRST) clear_flags(a, (int64_t)blockIdx.x * SORT_THREADS + threadIdx.x, (int64_t)gridDim.x * SORT_THREADS);
     __syncthreads();
     const int64_t items = FIRST ? a.items : a.counts[0];
     const int64_t begin = (int64_t)blockIdx.x * a.tile, end = min(items, begin + a.tile);
-    for (int64_t i = begin + threadIdx.x; i < end; i += SORT_THREADS) {
-        const int key = sort_key<FIRST>(a, i, end, a.dev_status);
-        if (key < 0) continue;
-        atomicAdd(&s_hist[(key >> a.shift) & (digits - 1)], 1);
-        if (FIRST && a.touched) {
-            const uint32_t bit = 1u << (key & 31);
-            if (!(a.touched[key >> 5] & bit)) atomicOr(&a.touched[key >> 5], bit);
-        }
+    for (int64_t r0 = begin; r0 < end; r0 += SORT_THREADS * SORT_ITEMS) {
+        int key[SORT_ITEMS], pos[SORT_ITEMS];
+        sort_keys<FIRST, SORT_ITEMS>(a, r0 + threadIdx.x, SORT_THREADS, end, true, key, pos);
+#pragma unroll
+        for (int u = 0; u < SORT_ITEMS; ++u)
+            if (key[u] >= 0) atomicAdd(&s_hist[(key[u] >> a.shift) & (digits - 1)], 1);
     }
     __syncthreads();
     for (int i = threadIdx.x; i < digits; i += SORT_THREADS) a.hist[(int64_t)blockIdx.x * digits + i] = s_hist[i];
 }
 
-template <bool FIRST>
+template <bool FIRST, int SORT_ITEMS>
 __global__ __launch_bounds__(SORT_THREADS) void sort_scatter_kernel(SortPass a) {
     __shared__ int s_base[MAX_DIGITS];                       // where the block's next item of each digit goes
     __shared__ int s_wave[SORT_WAVES][MAX_DIGITS];           // items of each digit per wave of a round
@@ -142,60 +203,29 @@ __global__ __launch_bounds__(SORT_THREADS) void sort_scatter_kernel(SortPass a) 
     const int digits = 1 << a.bits, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     // a thread per digit: items of that digit, and those of them that lie in earlier blocks
     static_assert(SORT_THREADS >= MAX_DIGITS, "a thread per digit");
-    int total = 0, before = 0;
+    int total = 0, mine = 0;
     if (tid < digits) {
-#pragma unroll 8
+        const int32_t* h = a.hist + tid;
+#pragma unroll 16
         for (int b = 0; b < a.blocks; ++b) {
-            const int h = a.hist[(int64_t)b * digits + tid];
-            total += h;
-            before += b < (int)blockIdx.x ? h : 0;
+            const int n = h[b << a.bits];
+            total += n;
+            mine += b < (int)blockIdx.x ? n : 0;
         }
     }
-    int run = total;                                         // inclusive sum over the digits
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int v = __shfl_up(run, o, 64);
-        if (lane >= o) run += v;
-    }
-    if (lane == 63) s_sum[wave] = run;
-    __syncthreads();
-    int lower = 0, all = 0;
-#pragma unroll
-    for (int w = 0; w < SORT_WAVES; ++w) {
-        if (w < wave) lower += s_sum[w];
-        all += s_sum[w];
-    }
-    if (tid < digits) s_base[tid] = lower + run - total + before;
+    int lower, all;
+    scan_threads<SORT_WAVES>(total, s_sum, lower, all);
+    if (tid < digits) s_base[tid] = lower + mine;
     if (FIRST && blockIdx.x == 0 && tid == 0) a.counts[0] = all;
     const int64_t items = FIRST ? a.items : all;
     const int64_t begin = (int64_t)blockIdx.x * a.tile, end = min(items, begin + a.tile);
     for (int64_t r0 = begin; r0 < end; r0 += SORT_THREADS * SORT_ITEMS) {
+        int key[SORT_ITEMS], pos[SORT_ITEMS], rank[SORT_ITEMS];
+        sort_keys<FIRST, SORT_ITEMS>(a, r0 + (int64_t)wave * 64 * SORT_ITEMS + lane, 64, end, false, key, pos);
         for (int i = tid; i < SORT_WAVES * digits; i += SORT_THREADS) s_wave[i >> a.bits][i & (digits - 1)] = 0;
-        int key[SORT_ITEMS], pos[SORT_ITEMS], rank[SORT_ITEMS] = {};
-        const int64_t first = r0 + (int64_t)wave * 64 * SORT_ITEMS + lane;
-#pragma unroll
-        for (int u = 0; u < SORT_ITEMS; ++u) {
-            key[u] = sort_key<FIRST>(a, first + u * 64, end, nullptr);
-            pos[u] = FIRST ? (int)(first + u * 64) : first + u * 64 < end ? a.pos_in[first + u * 64] : 0;
-        }
         __syncthreads();
 #pragma unroll
-        for (int u = 0; u < SORT_ITEMS; ++u) {
-            const int digit = (key[u] >> a.shift) & (digits - 1);
-            unsigned long long same = __ballot(key[u] >= 0);
-            for (int b = 0; b < a.bits; ++b) {
-                const unsigned long long votes = __ballot((digit >> b) & 1);
-                same &= ((digit >> b) & 1) ? votes : ~votes;
-            }
-            if (key[u] >= 0) {
-                const int ahead = __popcll(same & ((1ull << lane) - 1ull));
-                const int old = s_wave[wave][digit];         // the wave's own row: its lanes run in step
-                rank[u] = old + ahead;
-                __builtin_amdgcn_wave_barrier();
-                if (ahead == 0) s_wave[wave][digit] = old + __popcll(same);
-                __builtin_amdgcn_wave_barrier();
-            }
-        }
+        for (int u = 0; u < SORT_ITEMS; ++u) rank[u] = rank_in_wave(key[u], (key[u] >> a.shift) & (digits - 1), a.bits, s_wave[wave]);
         __syncthreads();
         if (tid < digits) {                                  // counts -> first places; the base moves on for the next round
             int at = s_base[tid];
@@ -219,117 +249,238 @@ __global__ __launch_bounds__(SORT_THREADS) void sort_scatter_kernel(SortPass a) 
     }
 }
 
+// The whole sort of a small batch in one block: the items stay in registers, and change places through the LDS after every pass.
+constexpr int ONE_WAVES = 16, ONE_THREADS = 64 * ONE_WAVES;
+template <int ONE_ITEMS>
+constexpr int one_block_lds() { return ONE_WAVES * MAX_DIGITS * 4 + ONE_THREADS * ONE_ITEMS * (4 + 2) + 64 * 4; }
+template <int ONE_ITEMS>
+__global__ __launch_bounds__(ONE_THREADS) void sort_one_block_kernel(SortPass a, int passes) {
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    int* const s_wave = (int*)lds;                            // [ONE_WAVES][digits]
+    int* const s_key = s_wave + ONE_WAVES * MAX_DIGITS;
+    uint16_t* const s_pos = (uint16_t*)(s_key + ONE_THREADS * ONE_ITEMS);
+    int* const s_sum = (int*)(s_pos + ONE_THREADS * ONE_ITEMS);
+    const int digits = 1 << a.bits, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int rounds = (int)((a.items + ONE_THREADS - 1) / ONE_THREADS), first = wave * rounds * 64 + lane;    // a wave's items lie next to each other
+    clear_flags(a, tid, ONE_THREADS);
+    int key[ONE_ITEMS], pos[ONE_ITEMS], rank[ONE_ITEMS];
+    uint8_t m[ONE_ITEMS];
+#pragma unroll
+    for (int u = 0; u < ONE_ITEMS; ++u) {
+        pos[u] = min(first + u * 64, (int)a.items - 1);
+        key[u] = u < rounds ? a.tokens[pos[u]] : -1;
+        m[u] = u < rounds && a.mask ? a.mask[pos[u]] : 1;
+    }
+    bool bad = false;
+#pragma unroll
+    for (int u = 0; u < ONE_ITEMS; ++u) {
+        const bool here = u < rounds && first + u * 64 < (int)a.items && m[u] != 0, in = key[u] >= 0 && key[u] < a.V;
+        bad |= here && !in;
+        if (!here || !in) key[u] = -1;
+    }
+    if (bad && a.dev_status) atomicOr(a.dev_status, RAPID_STATUS_BAD_TOKEN);
+    int items = 0;
+    for (int pass = 0; pass < passes; ++pass) {
+        const int shift = pass * a.bits;
+        for (int i = tid; i < ONE_WAVES * digits; i += ONE_THREADS) s_wave[i] = 0;
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < ONE_ITEMS; ++u) {
+            rank[u] = 0;
+            if (u < rounds) rank[u] = rank_in_wave(key[u], (key[u] >> shift) & (digits - 1), a.bits, s_wave + wave * digits);
+        }
+        __syncthreads();
+        int total = 0, lower;
+        if (tid < digits) {
+#pragma unroll
+            for (int w = 0; w < ONE_WAVES; ++w) total += s_wave[w * digits + tid];
+        }
+        scan_threads<ONE_WAVES>(total, s_sum, lower, items);
+        if (tid < digits) {
+#pragma unroll
+            for (int w = 0; w < ONE_WAVES; ++w) {
+                const int c = s_wave[w * digits + tid];
+                s_wave[w * digits + tid] = lower;
+                lower += c;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < ONE_ITEMS; ++u) {
+            if (key[u] < 0) continue;
+            const int at = s_wave[wave * digits + ((key[u] >> shift) & (digits - 1))] + rank[u];
+            s_key[at] = key[u];
+            s_pos[at] = (uint16_t)pos[u];
+        }
+        __syncthreads();
+        if (pass + 1 < passes) {
+#pragma unroll
+            for (int u = 0; u < ONE_ITEMS; ++u) {
+                const int i = first + u * 64;
+                const bool here = u < rounds && i < items;
+                key[u] = here ? s_key[i] : -1;
+                pos[u] = here ? s_pos[i] : 0;
+            }
+        }
+    }
+    for (int i = tid; i < items; i += ONE_THREADS) {
+        a.key_out[i] = s_key[i];
+        a.pos_out[i] = s_pos[i];
+    }
+    if (tid == 0) a.counts[0] = items;
+}
+
 // --------------------------------------------------------------------------------------------- sums
-// Sorted position i of the batch has id key[i].  A group of threads takes the `rows` sorted positions of one stretch, a thread one piece of
+// Sorted position i of the batch has id key[i].  A group of threads takes a stretch of sorted positions (the batch's valid positions shared out
+// evenly over at most `stretches` groups, which is about what the chip holds at once), a thread one piece of
 // the columns, and adds the gradient rows up in fp32; an id's sum that began and ended inside the stretch is the row of dE.  What crosses an end of the
 // stretch goes to `part`: slot 0 the sum that came in from before and ended here, slot 1 the one that goes on behind (it may have come in, too).  So the
 // work is shared out by rows whatever the ids are: one id that owns the whole batch is as quick as all ids different.
 struct SumArgs {
     const int32_t *key, *pos, *counts;
-    int64_t rows;           // per stretch
+    int64_t stretches, least_rows;
     int pieces;             // of a row
     float* part;            // [stretches][2][d]
+    uint8_t* flags;         // NULL (accumulate), or a byte per id that is set for those that occur
     int64_t d;
     float scale;
-    int accumulate;
 };
+__device__ __forceinline__ int64_t stretch_rows(const SumArgs& a, int64_t M) { return max(a.least_rows, (M + a.stretches - 1) / a.stretches); }
 
-template <class P, class D>
-__device__ __forceinline__ void store_row(D* __restrict__ at, const float (&acc)[P::N], float scale, int accumulate) {
+template <class P, class D, bool ACC>
+__device__ __forceinline__ void store_row(D* __restrict__ at, const float (&acc)[P::N], const float (&old)[ACC ? P::N : 1], float scale) {
     constexpr int N = P::N;
+    float f[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) f[e] = ACC ? fmaf(acc[e], scale, old[ACC ? e : 0]) : acc[e] * scale;
     if constexpr (sizeof(D) == 4 && N == 1) {
-        at[0] = accumulate ? fmaf(acc[0], scale, at[0]) : acc[0] * scale;
+        at[0] = f[0];
     } else if constexpr (sizeof(D) == 4) {
 #pragma unroll
-        for (int q = 0; q < N / 4; ++q) {
-            float4* to = (float4*)at + q;
-            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (accumulate) v = *to;
-            *to = make_float4(fmaf(acc[4 * q], scale, v.x), fmaf(acc[4 * q + 1], scale, v.y), fmaf(acc[4 * q + 2], scale, v.z),
-                              fmaf(acc[4 * q + 3], scale, v.w));
-        }
+        for (int q = 0; q < N / 4; ++q) ((float4*)at)[q] = make_float4(f[4 * q], f[4 * q + 1], f[4 * q + 2], f[4 * q + 3]);
     } else if constexpr (N == 8) {
-        float f[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = acc[e] * scale;
         *(uint4*)at = pack8(f);
     } else if constexpr (N == 4) {
-        *(uint2*)at = make_uint2(pack2(acc[0] * scale, acc[1] * scale), pack2(acc[2] * scale, acc[3] * scale));
+        *(uint2*)at = make_uint2(pack2(f[0], f[1]), pack2(f[2], f[3]));
     } else {
-        at[0] = __builtin_bit_cast(bf16_t, (__bf16)(acc[0] * scale));
+        at[0] = __builtin_bit_cast(bf16_t, (__bf16)f[0]);
+    }
+}
+template <class P, class D, bool ACC>
+__device__ __forceinline__ void load_row(const D* __restrict__ at, float (&old)[ACC ? P::N : 1]) {
+    if constexpr (ACC && P::N == 1) old[0] = at[0];
+    else if constexpr (ACC) {
+#pragma unroll
+        for (int q = 0; q < P::N / 4; ++q) {
+            const float4 v = ((const float4*)at)[q];
+            old[4 * q] = v.x; old[4 * q + 1] = v.y; old[4 * q + 2] = v.z; old[4 * q + 3] = v.w;
+        }
     }
 }
 
-template <class P, class D>
+// U rows under way together; with ACC also the old values of the rows that end among them.  The next batch's ids and positions are asked for
+// before this batch's rows are waited for.  WAVES: groups are whole waves, ids and positions scalars (104 registers a thread without, RESULT with:
+// twice as many waves fit).
+template <class P, class D, bool ACC, bool WAVES>
 __global__ __launch_bounds__(256) void embedding_sum_kernel(SumArgs a, const typename P::elem* __restrict__ dh, D* __restrict__ dE) {
     typedef typename P::raw raw;
-    const int64_t M = a.counts[0];
-    const int64_t s = (int64_t)blockIdx.x * blockDim.y + threadIdx.y, begin = s * a.rows;
-    if (begin >= M) return;
-    const int64_t end = min(M, begin + a.rows);
-    const raw* src = (const raw*)dh;
-    constexpr int U = 8;
-    for (int piece = blockIdx.y * blockDim.x + threadIdx.x; piece < a.pieces; piece += gridDim.y * blockDim.x) {
-        float acc[P::N];
+    constexpr int U = ACC ? 4 : 8;
+    const int64_t M = a.counts[0], rows = stretch_rows(a, M);
+    const int group = WAVES ? __builtin_amdgcn_readfirstlane(threadIdx.y) : threadIdx.y;
+    const int64_t s = (int64_t)blockIdx.x * blockDim.y + group, begin = s * rows;
+    const int piece = blockIdx.y * blockDim.x + threadIdx.x;
+    if (begin >= M || piece >= a.pieces) return;
+    const int64_t end = min(M, begin + rows);
+    const raw* src = (const raw*)dh + piece;
+    float acc[P::N];
 #pragma unroll
-        for (int e = 0; e < P::N; ++e) acc[e] = 0.f;
-        bool came_in = begin > 0 && a.key[begin - 1] == a.key[begin];
-        for (int64_t i0 = begin; i0 < end; i0 += U) {
-            raw v[U];
-            int k[U + 1];
+    for (int e = 0; e < P::N; ++e) acc[e] = 0.f;
+    const int behind = end < M ? a.key[end] : -1;
+    bool came_in = begin > 0 && a.key[begin - 1] == a.key[begin];
+    int k[U], p[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int64_t i = i0 + u < end ? i0 + u : end - 1;
-                k[u] = a.key[i];
-                v[u] = src[(int64_t)a.pos[i] * a.pieces + piece];
-            }
-            k[U] = i0 + U < M ? a.key[i0 + U] : -1;
+    for (int u = 0; u < U; ++u) {
+        const int64_t i = min(begin + u, end - 1);
+        k[u] = a.key[i];
+        p[u] = a.pos[i];
+    }
+    for (int64_t i0 = begin; i0 < end; i0 += U) {
+        raw v[U];
+        float old[U][ACC ? P::N : 1];
+        int kn[U], pn[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int64_t i = i0 + u;
-                if (i >= end) break;
-                float f[P::N];
-                P::get(v[u], f);
+        for (int u = 0; u < U; ++u) v[u] = src[(int64_t)p[u] * a.pieces];
 #pragma unroll
-                for (int e = 0; e < P::N; ++e) acc[e] += f[e];
-                const int next = i + 1 < end ? k[u + 1] : end < M ? a.key[end] : -1;
-                if (next == k[u] && i + 1 < end) continue;
-                const bool goes_on = next == k[u];
-                if (came_in || goes_on) {
-                    float* to = a.part + (s * 2 + (goes_on ? 1 : 0)) * a.d + (int64_t)piece * P::N;
-#pragma unroll
-                    for (int e = 0; e < P::N; ++e) to[e] = acc[e];
-                } else {
-                    store_row<P, D>(dE + (int64_t)k[u] * a.d + (int64_t)piece * P::N, acc, a.scale, a.accumulate);
-                }
-                came_in = false;
-#pragma unroll
-                for (int e = 0; e < P::N; ++e) acc[e] = 0.f;
-            }
+        for (int u = 0; u < U; ++u) {
+            const int64_t i = min(i0 + U + u, end - 1);
+            kn[u] = a.key[i];
+            pn[u] = a.pos[i];
         }
+        auto next_of = [&](int u) { return i0 + u + 1 >= end ? behind : u + 1 < U ? k[u + 1] : kn[0]; };
+        if constexpr (ACC) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (next_of(u) != k[u]) load_row<P, D, ACC>(dE + (int64_t)k[u] * a.d + (int64_t)piece * P::N, old[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (i0 + u >= end) break;
+            float f[P::N];
+            P::get(v[u], f);
+#pragma unroll
+            for (int e = 0; e < P::N; ++e) acc[e] += f[e];
+            const bool last = i0 + u + 1 == end, goes_on = next_of(u) == k[u];
+            if (goes_on && !last) continue;
+            if (came_in || goes_on) {
+                float* to = a.part + (s * 2 + (goes_on ? 1 : 0)) * a.d + (int64_t)piece * P::N;
+#pragma unroll
+                for (int e = 0; e < P::N; ++e) to[e] = acc[e];
+            } else {
+                store_row<P, D, ACC>(dE + (int64_t)k[u] * a.d + (int64_t)piece * P::N, acc, old[u], a.scale);
+            }
+            if (!ACC && piece == 0) a.flags[k[u]] = 1;
+            came_in = false;
+#pragma unroll
+            for (int e = 0; e < P::N; ++e) acc[e] = 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) { k[u] = kn[u]; p[u] = pn[u]; }
     }
 }
 
 // Joins the sums that crossed ends of stretches: the block of the stretch in which such an id began adds up what the stretches after it left, in
-// order (in MERGE_WAVES consecutive shares, then these in order).
-constexpr int MERGE_WAVES = 8;
-template <class P, class D>
-__global__ __launch_bounds__(64 * MERGE_WAVES) void embedding_merge_kernel(SumArgs a, D* __restrict__ dE) {
+// order (in MERGE_WAVES consecutive shares, then these in order).  The blocks behind those of the stretches clear the rows of the ids that do
+// not occur, ZERO_ROWS of them a wave.
+constexpr int MERGE_WAVES = 8, ZERO_ROWS = 16;
+template <class P, class D, bool ACC, class W>
+__global__ __launch_bounds__(64 * MERGE_WAVES) void embedding_merge_kernel(SumArgs a, D* __restrict__ dE, int64_t V, int64_t row_words) {
     __shared__ float s_sum[MERGE_WAVES][64][P::N];
-    const int64_t M = a.counts[0], s = blockIdx.x, begin = s * a.rows, end = begin + a.rows;
-    if (end >= M) return;                                   // nothing goes on behind the last stretch
-    const int key = a.key[end - 1];
-    if (a.key[end] != key) return;
-    if (a.key[begin] == key && begin > 0 && a.key[begin - 1] == key) return;      // began in an earlier stretch
-    int64_t lo = end, hi = M;                               // first sorted position behind the id's
-    while (lo < hi) {
-        const int64_t mid = (lo + hi) >> 1;
-        if (a.key[mid] == key) lo = mid + 1; else hi = mid;
-    }
-    const int64_t last = (lo - 1) / a.rows;                 // stretches s .. last; the sum ended in the last one: slot 0 there
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t s = blockIdx.x;
+    if (!ACC && s >= a.stretches - 1) {
+        const int64_t v0 = ((s - (a.stretches - 1)) * MERGE_WAVES + wave) * ZERO_ROWS;
+        unsigned long long rows = __ballot(lane < ZERO_ROWS && v0 + lane < V && a.flags[v0 + lane] == 0);
+        for (; rows; rows &= rows - 1) {
+            W* row = (W*)dE + (v0 + __ffsll((long long)rows) - 1) * row_words;
+            for (int64_t i = lane; i < row_words; i += 64) row[i] = W{};
+        }
+        return;
+    }
+    const int64_t M = a.counts[0], n_rows = stretch_rows(a, M), begin = s * n_rows, end = begin + n_rows;
+    if (end >= M) return;                                   // nothing goes on behind the last stretch
+    // (the keys are asked for together)
+    const int key = a.key[end - 1], key_behind = a.key[end], key_first = a.key[begin], key_before = a.key[begin > 0 ? begin - 1 : 0];
+    if (key_behind != key) return;
+    if (key_first == key && begin > 0 && key_before == key) return;      // began in an earlier stretch
+    int64_t last = s + 1;                                   // the stretch in which the id's run ends: 64 are looked at together
+    for (;; last += 64) {
+        const int64_t at = (last + lane + 1) * n_rows - 1;
+        const unsigned long long other = __ballot(at >= M - 1 || a.key[at < M ? at : M - 1] != key);
+        if (other) { last += __ffsll((long long)other) - 1; break; }
+    }
+    if (a.key[last * n_rows] != key) --last;                // it ended with the stretch before (its sum there is in slot 0 all the same)
     const int64_t n = last - s + 1, from = s + n * wave / MERGE_WAVES, to = s + n * (wave + 1) / MERGE_WAVES;
-    for (int piece0 = blockIdx.y * 64; piece0 < a.pieces; piece0 += gridDim.y * 64) {
+    for (int piece0 = 0; piece0 < a.pieces; piece0 += 64) {
         const int piece = piece0 + lane;
         float acc[P::N];
 #pragma unroll
@@ -349,58 +500,66 @@ __global__ __launch_bounds__(64 * MERGE_WAVES) void embedding_merge_kernel(SumAr
             for (int w = 1; w < MERGE_WAVES; ++w)
 #pragma unroll
                 for (int e = 0; e < P::N; ++e) acc[e] += s_sum[w][lane][e];
-            store_row<P, D>(dE + (int64_t)key * a.d + (int64_t)piece * P::N, acc, a.scale, a.accumulate);
+            D* to_row = dE + (int64_t)key * a.d + (int64_t)piece * P::N;
+            float old[ACC ? P::N : 1];
+            load_row<P, D, ACC>(to_row, old);
+            store_row<P, D, ACC>(to_row, acc, old, a.scale);
         }
         __syncthreads();
     }
 }
 
-// rows of ids that do not occur
-template <class W>
-__global__ __launch_bounds__(256) void embedding_zero_kernel(const uint32_t* __restrict__ touched, int64_t V, int64_t words, W* __restrict__ dE) {
-    for (int64_t v = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6); v < V; v += (int64_t)gridDim.x * 4) {
-        if ((touched[v >> 5] >> (v & 31)) & 1u) continue;
-        for (int64_t i = threadIdx.x & 63; i < words; i += 64) dE[v * words + i] = W{};
-    }
-}
-
-__global__ void zero_words_kernel(uint32_t* __restrict__ p, int64_t n) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (i < n) p[i] = 0u;
-}
-
-template <class P, class D>
-void sum_t(const EmbeddingArgs& a, const SumArgs& s, int64_t stretches, const void* dh, D* dE, hipStream_t st) {
-    // a group of threads for a stretch: enough of them for a row's pieces, up to a block
+// threads of a group: enough of them for a row's pieces, up to a block
+int group_threads(int64_t pieces) {
+    if (pieces > 64) return pieces >= 256 ? 256 : (int)((pieces + 63) / 64 * 64);
     int x = 8;
-    while (x < 64 && x < s.pieces) x *= 2;
-    if (s.pieces > 64) x = s.pieces >= 256 ? 256 : (s.pieces + 63) / 64 * 64;
-    const int y = 256 / x;
-    const int64_t columns = (s.pieces + x - 1) / x;
-    embedding_sum_kernel<P, D><<<dim3((unsigned)((stretches + y - 1) / y), (unsigned)columns), dim3(x, y), 0, st>>>(s, (const typename P::elem*)dh, dE);
-    if (stretches > 1)
-        embedding_merge_kernel<P, D><<<dim3((unsigned)(stretches - 1), (unsigned)((s.pieces + 63) / 64)), 64 * MERGE_WAVES, 0, st>>>(s, dE);
+    while (x < pieces) x *= 2;
+    return x;
 }
 
-template <class D>
-void bwd_t(const EmbeddingArgs& a, SumArgs s, const uint32_t* touched, int64_t stretches, const void* dh, D* dE, hipStream_t st) {
-    if (!s.accumulate) {
-        const int64_t bytes = a.d * (int64_t)sizeof(D);
-        const unsigned grid = (unsigned)((a.V + 3) / 4 < 8192 ? (a.V + 3) / 4 : 8192);
-        if (bytes % 16 == 0) embedding_zero_kernel<uint4><<<grid, 256, 0, st>>>(touched, a.V, bytes / 16, (uint4*)dE);
-        else embedding_zero_kernel<D><<<grid, 256, 0, st>>>(touched, a.V, a.d, dE);
-    }
-    if (a.dtype == RAPID_DTYPE_BF16) sum_t<BF16x8, D>(a, s, stretches, dh, dE, st);
-    else if (a.d % 4 == 0) sum_t<F32x4, D>(a, s, stretches, dh, dE, st);
-    else sum_t<F32x1, D>(a, s, stretches, dh, dE, st);
+template <class P, class D, bool ACC, class W>
+void sum_t(const SumArgs& s, int64_t V, int64_t row_words, const void* dh, D* dE, hipStream_t st) {
+    const int x = group_threads(s.pieces), y = 256 / x;
+    const dim3 grid((unsigned)((s.stretches + y - 1) / y), (unsigned)((s.pieces + x - 1) / x)), block(x, y);
+    if (x % 64 == 0) embedding_sum_kernel<P, D, ACC, true><<<grid, block, 0, st>>>(s, (const typename P::elem*)dh, dE);
+    else embedding_sum_kernel<P, D, ACC, false><<<grid, block, 0, st>>>(s, (const typename P::elem*)dh, dE);
+    const int64_t blocks = s.stretches - 1 + (ACC ? 0 : (V + MERGE_WAVES * ZERO_ROWS - 1) / (MERGE_WAVES * ZERO_ROWS));
+    if (blocks > 0) embedding_merge_kernel<P, D, ACC, W><<<(unsigned)blocks, 64 * MERGE_WAVES, 0, st>>>(s, dE, V, row_words);
+}
+template <class P, class D>
+void sum_d(const SumArgs& s, int64_t V, const void* dh, D* dE, hipStream_t st) {
+    if constexpr (sizeof(D) == 4)
+        if (!s.flags) { sum_t<P, D, true, D>(s, V, 0, dh, dE, st); return; }
+    const int64_t bytes = s.d * (int64_t)sizeof(D);
+    if (bytes % 16 == 0) sum_t<P, D, false, uint4>(s, V, bytes / 16, dh, dE, st);
+    else sum_t<P, D, false, D>(s, V, s.d, dh, dE, st);
 }
 
+int pieces_of(int64_t d, int dtype) { return (int)(d / (dtype == RAPID_DTYPE_BF16 ? 8 : d % 4 == 0 ? 4 : 1)); }
+
+// Items a thread takes in a round of the sort.  Few positions: more blocks with less to do each.
+constexpr int FEW_ITEMS = 2, MANY_ITEMS = 8;
+constexpr int64_t FEW_POSITIONS = 131072, ONE_BLOCK_SORT = 8192;
 int64_t sort_tile(int64_t positions) {
-    constexpr int64_t round = SORT_THREADS * SORT_ITEMS;
+    const int64_t round = SORT_THREADS * (positions <= FEW_POSITIONS ? FEW_ITEMS : MANY_ITEMS);
     const int64_t per = (positions + 255) / 256;            // at most 256 blocks: every block adds up the counts of all
     return (per + round - 1) / round * round;
 }
-int64_t stretch_rows(int64_t positions) { return positions <= 32768 ? 16 : positions <= 262144 ? 64 : positions <= ((int64_t)1 << 24) ? 128 : 1024; }
+template <int ITEMS>
+void sort_one_t(const SortPass& s, int passes, hipStream_t st) {
+    allow_lds<&sort_one_block_kernel<ITEMS>>(one_block_lds<ITEMS>());
+    sort_one_block_kernel<ITEMS><<<1, ONE_THREADS, one_block_lds<ITEMS>(), st>>>(s, passes);
+}
+template <int ITEMS>
+void sort_pass_t(const SortPass& s, hipStream_t st) {
+    if (s.shift == 0) {
+        sort_count_kernel<true, ITEMS><<<(unsigned)s.blocks, SORT_THREADS, 0, st>>>(s);
+        sort_scatter_kernel<true, ITEMS><<<(unsigned)s.blocks, SORT_THREADS, 0, st>>>(s);
+    } else {
+        sort_count_kernel<false, ITEMS><<<(unsigned)s.blocks, SORT_THREADS, 0, st>>>(s);
+        sort_scatter_kernel<false, ITEMS><<<(unsigned)s.blocks, SORT_THREADS, 0, st>>>(s);
+    }
+}
 
 }  // namespace
 
@@ -410,7 +569,7 @@ void launch_embedding_fwd(const EmbeddingArgs& a, const void* table, void* out, 
     else fwd_t<F32x1>(a, table, out, st);
 }
 
-EmbeddingPlan embedding_plan(int64_t positions, int64_t d, int64_t V) {
+EmbeddingPlan embedding_plan(int64_t positions, int64_t d, int64_t V, int dtype) {
     EmbeddingPlan p;
     int bits = 1;
     while (((int64_t)1 << bits) < V) ++bits;
@@ -418,8 +577,12 @@ EmbeddingPlan embedding_plan(int64_t positions, int64_t d, int64_t V) {
     p.bits = (bits + p.passes - 1) / p.passes;
     p.tile = sort_tile(positions);
     p.blocks = (positions + p.tile - 1) / p.tile;
-    p.rows = stretch_rows(positions);
-    p.stretches = (positions + p.rows - 1) / p.rows;
+    // 32 waves per CU, 4 rows at least a group
+    p.least_rows = 4;
+    const int64_t pieces = pieces_of(d, dtype), x = group_threads(pieces), held = (int64_t)8192 * 64 / ((pieces + x - 1) / x * x);
+    const int64_t wanted = (positions + p.least_rows - 1) / p.least_rows;
+    p.stretches = wanted < held ? wanted : held < 64 ? 64 : held;
+    if (p.stretches > wanted) p.stretches = wanted;
     size_t cur = 0;
     auto take = [&](size_t bytes) { const size_t at = cur; cur += (bytes + 255) / 256 * 256; return at; };
     p.counts = take(64 * 4);
@@ -428,7 +591,7 @@ EmbeddingPlan embedding_plan(int64_t positions, int64_t d, int64_t V) {
         p.pos[i] = take((size_t)positions * 4);
     }
     p.hist = take((size_t)p.blocks * (1u << p.bits) * 4);
-    p.touched = take((size_t)((V + 31) / 32) * 4);
+    p.flags = take((size_t)V);
     p.part = take((size_t)p.stretches * 2 * (size_t)d * 4);
     p.total = cur;
     return p;
@@ -436,35 +599,37 @@ EmbeddingPlan embedding_plan(int64_t positions, int64_t d, int64_t V) {
 
 void launch_embedding_bwd(const EmbeddingArgs& a, const EmbeddingPlan& p, void* ws, const void* dh, int dw_dtype, int accumulate, void* dE, hipStream_t st) {
     char* w = (char*)ws;
-    uint32_t* touched = accumulate ? nullptr : (uint32_t*)(w + p.touched);
-    if (touched) {
-        const int64_t words = (a.V + 31) / 32;
-        zero_words_kernel<<<(unsigned)((words + 255) / 256), 256, 0, st>>>(touched, words);
-    }
     SortPass s{};
     s.tokens = a.tokens; s.mask = a.mask; s.V = (int)a.V; s.dev_status = a.dev_status;
-    s.hist = (int32_t*)(w + p.hist); s.counts = (int32_t*)(w + p.counts); s.touched = touched;
+    s.hist = (int32_t*)(w + p.hist); s.counts = (int32_t*)(w + p.counts);
+    s.flags = accumulate ? nullptr : (uint32_t*)(w + p.flags); s.flag_words = (a.V + 3) / 4;
     s.items = a.positions; s.tile = p.tile; s.bits = p.bits; s.blocks = (int)p.blocks;
-    const unsigned grid = (unsigned)p.blocks;
-    for (int pass = 0; pass < p.passes; ++pass) {
-        const int to = pass & 1;
-        s.shift = pass * p.bits;
-        s.key_in = (const int32_t*)(w + p.key[to ^ 1]); s.pos_in = (const int32_t*)(w + p.pos[to ^ 1]);
-        s.key_out = (int32_t*)(w + p.key[to]); s.pos_out = (int32_t*)(w + p.pos[to]);
-        if (pass == 0) {
-            sort_count_kernel<true><<<grid, SORT_THREADS, 0, st>>>(s);
-            sort_scatter_kernel<true><<<grid, SORT_THREADS, 0, st>>>(s);
-        } else {
-            sort_count_kernel<false><<<grid, SORT_THREADS, 0, st>>>(s);
-            sort_scatter_kernel<false><<<grid, SORT_THREADS, 0, st>>>(s);
+    if (a.positions <= ONE_BLOCK_SORT) {
+        s.key_out = (int32_t*)(w + p.key[0]); s.pos_out = (int32_t*)(w + p.pos[0]);
+        if (a.positions <= ONE_THREADS) sort_one_t<1>(s, p.passes, st);
+        else if (a.positions <= 4 * ONE_THREADS) sort_one_t<4>(s, p.passes, st);
+        else sort_one_t<8>(s, p.passes, st);
+    } else {
+        for (int pass = 0; pass < p.passes; ++pass) {
+            const int to = pass & 1;
+            s.shift = pass * p.bits;
+            s.key_in = (const int32_t*)(w + p.key[to ^ 1]); s.pos_in = (const int32_t*)(w + p.pos[to ^ 1]);
+            s.key_out = (int32_t*)(w + p.key[to]); s.pos_out = (int32_t*)(w + p.pos[to]);
+            if (a.positions <= FEW_POSITIONS) sort_pass_t<FEW_ITEMS>(s, st);
+            else sort_pass_t<MANY_ITEMS>(s, st);
         }
     }
     SumArgs u{};
-    u.key = s.key_out; u.pos = s.pos_out; u.counts = s.counts; u.rows = p.rows;
-    u.pieces = (int)(a.d / (a.dtype == RAPID_DTYPE_BF16 ? 8 : a.d % 4 == 0 ? 4 : 1));
-    u.part = (float*)(w + p.part); u.d = a.d; u.scale = a.scale; u.accumulate = accumulate;
-    if (dw_dtype == RAPID_DTYPE_F32) bwd_t<float>(a, u, touched, p.stretches, dh, (float*)dE, st);
-    else bwd_t<bf16_t>(a, u, touched, p.stretches, dh, (bf16_t*)dE, st);
+    u.key = s.key_out; u.pos = s.pos_out; u.counts = s.counts; u.stretches = p.stretches; u.least_rows = p.least_rows;
+    u.pieces = pieces_of(a.d, a.dtype);
+    u.part = (float*)(w + p.part); u.flags = (uint8_t*)s.flags; u.d = a.d; u.scale = a.scale;
+    auto go = [&](auto* out) {
+        if (a.dtype == RAPID_DTYPE_BF16) sum_d<BF16x8>(u, a.V, dh, out, st);
+        else if (a.d % 4 == 0) sum_d<F32x4>(u, a.V, dh, out, st);
+        else sum_d<F32x1>(u, a.V, dh, out, st);
+    };
+    if (dw_dtype == RAPID_DTYPE_F32) go((float*)dE);
+    else go((bf16_t*)dE);
 }
 
 }  // namespace rapid

@@ -929,7 +929,7 @@ int64_t rapid_logits_cache_rows(int64_t N, int64_t T, int64_t d, int64_t V, int6
 // calls whose workspace has one size
 static size_t one_size_workspace(int op, int64_t N, int64_t T, int64_t d, int64_t V, int dtype) {
     if ((dtype != RAPID_DTYPE_F32 && dtype != RAPID_DTYPE_BF16) || !table_shape(N, T, d, V)) return 0;
-    if (op == RAPID_OP_EMBEDDING_BWD) return embedding_plan(N * T, d, V).total;
+    if (op == RAPID_OP_EMBEDDING_BWD) return embedding_plan(N * T, d, V, dtype).total;
     Fp8Plan p;
     return make_fp8_plan(p, N, T, d, V) ? p.total : 0;
 }
@@ -1062,7 +1062,7 @@ int rapid_embedding_bwd(const void* dhidden, const int32_t* tokens, const uint8_
         set_error("rapid_embedding_bwd: dw_dtype %d (a gradient is added to in fp32 only)", dw_dtype);
         return RAPID_ERR_DTYPE;
     }
-    const EmbeddingPlan p = embedding_plan(N * T, d, V);
+    const EmbeddingPlan p = embedding_plan(N * T, d, V, dtype);
     rc = validate_workspace("rapid_embedding_bwd", workspace, workspace_bytes, p.total);
     if (!rc) rc = check_arch();
     if (rc) return rc;

@@ -408,10 +408,10 @@ void launch_embedding_fwd(const EmbeddingArgs& a, const void* table, void* out, 
 struct EmbeddingPlan {
     int passes, bits;                  // radix passes and bits of the id in each
     int64_t tile, blocks;              // positions per block of a pass
-    int64_t rows, stretches;           // sorted positions that a group of threads adds up
-    size_t counts, key[2], pos[2], hist, touched, part, total;
+    int64_t stretches, least_rows;     // groups of threads that share the sorted positions, and what a group gets at least
+    size_t counts, key[2], pos[2], hist, flags, part, total;
 };
-EmbeddingPlan embedding_plan(int64_t positions, int64_t d, int64_t V);
+EmbeddingPlan embedding_plan(int64_t positions, int64_t d, int64_t V, int dtype);
 void launch_embedding_bwd(const EmbeddingArgs& a, const EmbeddingPlan& p, void* ws, const void* dh, int dw_dtype, int accumulate, void* dE, hipStream_t st);
 
 // ---- probe.hip -----------------------------------------------------------------------------------
