@@ -24,6 +24,26 @@ struct F32x1 { static constexpr int N = 1; typedef float elem; typedef float raw
     static __device__ __forceinline__ void get(const raw& v, float (&f)[1]) { f[0] = v; }
     static __device__ __forceinline__ raw put(const float (&f)[1]) { return f[0]; } };
 
+// 16 bytes (or an element) that nobody reads before they have left the caches: stored past them, read without keeping them
+template <class R>
+__device__ __forceinline__ void store_past(R* to, const R& v) {
+    if constexpr (sizeof(R) == 16) {
+        typedef unsigned u4 __attribute__((ext_vector_type(4)));
+        __builtin_nontemporal_store(__builtin_bit_cast(u4, v), (u4*)to);
+    } else {
+        __builtin_nontemporal_store(v, to);
+    }
+}
+template <class R>
+__device__ __forceinline__ R load_once(const R* from) {
+    if constexpr (sizeof(R) == 16) {
+        typedef unsigned u4 __attribute__((ext_vector_type(4)));
+        return __builtin_bit_cast(R, __builtin_nontemporal_load((const u4*)from));
+    } else {
+        return __builtin_nontemporal_load(from);
+    }
+}
+
 // token at position p, or -1 where it has no row: masked, or (flagged) out of range
 __device__ __forceinline__ int valid_token(const int32_t* __restrict__ tokens, const uint8_t* __restrict__ mask, int64_t p, int V,
                                            int32_t* __restrict__ dev_status) {
@@ -37,8 +57,9 @@ __device__ __forceinline__ int valid_token(const int32_t* __restrict__ tokens, c
 // ------------------------------------------------------------------------------------------- lookup
 // A wave takes `rows` consecutive positions (at most 64; its lanes hold their ids) and walks their pieces side by side: lane l has pieces
 // l, l + 64, ... of the run of rows, so no lane idles where a row is no multiple of 64 pieces.  (row, piece) advance by 64 pieces =
-// step_rows rows and step_pieces pieces.
-template <class P>
+// step_rows rows and step_pieces pieces.  PAST: the output is larger than the memory-side cache, which is left to the table (256 x 2048 x 1536 bf16: 505 us
+// without, 394 with).
+template <class P, bool PAST, int U>
 __global__ __launch_bounds__(256) void embedding_fwd_kernel(const typename P::elem* __restrict__ table, const int32_t* __restrict__ tokens,
                                                             const uint8_t* __restrict__ mask, int64_t positions, int pieces, int V,
                                                             float scale, typename P::elem* __restrict__ out,
@@ -52,14 +73,14 @@ __global__ __launch_bounds__(256) void embedding_fwd_kernel(const typename P::el
     int row = lane / pieces, piece = lane - row * pieces;
     raw* dst = (raw*)out + p0 * pieces;
     const raw* src = (const raw*)table;
-    constexpr int U = 4;
     for (int base = 0; base < n * pieces; base += 64 * U) {
         raw v[U];
         int t[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             t[u] = __shfl(tok, row < n ? row : 0, 64);
-            v[u] = src[(int64_t)(t[u] < 0 ? 0 : t[u]) * pieces + piece];
+            v[u] = raw{};
+            if (t[u] >= 0) v[u] = src[(int64_t)t[u] * pieces + piece];
             row += step_rows;
             piece += step_pieces;
             if (piece >= pieces) { piece -= pieces; ++row; }
@@ -72,20 +93,31 @@ __global__ __launch_bounds__(256) void embedding_fwd_kernel(const typename P::el
             P::get(v[u], f);
 #pragma unroll
             for (int e = 0; e < P::N; ++e) f[e] = t[u] < 0 ? 0.f : f[e] * scale;
-            dst[i] = P::put(f);
+            if (PAST) store_past(dst + i, P::put(f));
+            else dst[i] = P::put(f);
         }
     }
 }
 
+constexpr int64_t BEYOND_CACHES = (int64_t)256 << 20;      // bytes of the memory-side cache
 template <class P>
 void fwd_t(const EmbeddingArgs& a, const void* table, void* out, hipStream_t st) {
     const int pieces = (int)(a.d / P::N);
-    // few positions: a wave for each, so that all are under way together
-    const int rows = a.positions <= 16384 ? 1 : a.positions <= ((int64_t)1 << 26) ? 8 : 64;     // a launch holds less than 2^32 threads
+    // A wave takes a row, in trips of U pieces a lane with as few lanes left over as can be, or the rows that make up a trip of 4.  (256 x 2048 x 1536,
+    // 3 pieces a lane, cold tables: U = 3 387 us, U = 4 411; 2, 4 and 8 rows a wave with U = 3: 385, 416, 454.)  A launch holds less than 2^32 threads.
+    const int trips = (pieces + 63) / 64;
+    int rows = 256 / pieces < 1 ? 1 : trips > 1 ? 1 : 256 / pieces > 64 ? 64 : 256 / pieces;
+    if (a.positions <= 16384) rows = 1;                     // few: all under way together
+    if (a.positions > ((int64_t)1 << 25)) rows = 64;
     const int64_t waves = (a.positions + rows - 1) / rows;
-    embedding_fwd_kernel<P><<<(unsigned)((waves + 3) / 4), 256, 0, st>>>(
-        (const typename P::elem*)table, a.tokens, a.mask, a.positions, pieces, (int)a.V, a.scale, (typename P::elem*)out, a.dev_status, rows,
-        64 / pieces, 64 % pieces);
+    const bool past = a.positions * a.d * (int64_t)sizeof(typename P::elem) > BEYOND_CACHES;
+    auto go = [&](auto* kernel) {
+        kernel<<<(unsigned)((waves + 3) / 4), 256, 0, st>>>((const typename P::elem*)table, a.tokens, a.mask, a.positions, pieces, (int)a.V, a.scale,
+                                                             (typename P::elem*)out, a.dev_status, rows, 64 / pieces, 64 % pieces);
+    };
+    if (trips == 2) past ? go(&embedding_fwd_kernel<P, true, 2>) : go(&embedding_fwd_kernel<P, false, 2>);
+    else if (trips > 1 && (trips + 2) / 3 * 3 < (trips + 3) / 4 * 4) past ? go(&embedding_fwd_kernel<P, true, 3>) : go(&embedding_fwd_kernel<P, false, 3>);
+    else past ? go(&embedding_fwd_kernel<P, true, 4>) : go(&embedding_fwd_kernel<P, false, 4>);
 }
 
 // --------------------------------------------------------------------------------------------- sort
@@ -344,6 +376,7 @@ struct SumArgs {
     uint8_t* flags;         // NULL (accumulate), or a byte per id that is set for those that occur
     int64_t d;
     float scale;
+    int once;               // the gradient rows are more than the caches hold: read past them (256 x 2048 x 1536 bf16: sums 273 -> 237 us)
 };
 __device__ __forceinline__ int64_t stretch_rows(const SumArgs& a, int64_t M) { return max(a.least_rows, (M + a.stretches - 1) / a.stretches); }
 
@@ -379,8 +412,7 @@ __device__ __forceinline__ void load_row(const D* __restrict__ at, float (&old)[
 }
 
 // U rows under way together; with ACC also the old values of the rows that end among them.  The next batch's ids and positions are asked for
-// before this batch's rows are waited for.  WAVES: groups are whole waves, ids and positions scalars (104 registers a thread without, RESULT with:
-// twice as many waves fit).
+// before this batch's rows are waited for.  WAVES: groups are whole waves, ids and positions scalars (104 registers a thread without, 70 with).
 template <class P, class D, bool ACC, bool WAVES>
 __global__ __launch_bounds__(256) void embedding_sum_kernel(SumArgs a, const typename P::elem* __restrict__ dh, D* __restrict__ dE) {
     typedef typename P::raw raw;
@@ -408,8 +440,13 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(SumArgs a, const typ
         raw v[U];
         float old[U][ACC ? P::N : 1];
         int kn[U], pn[U];
+        if (a.once) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) v[u] = src[(int64_t)p[u] * a.pieces];
+            for (int u = 0; u < U; ++u) v[u] = load_once(src + (int64_t)p[u] * a.pieces);
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u) v[u] = src[(int64_t)p[u] * a.pieces];
+        }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int64_t i = min(i0 + U + u, end - 1);
@@ -577,9 +614,9 @@ EmbeddingPlan embedding_plan(int64_t positions, int64_t d, int64_t V, int dtype)
     p.bits = (bits + p.passes - 1) / p.passes;
     p.tile = sort_tile(positions);
     p.blocks = (positions + p.tile - 1) / p.tile;
-    // 32 waves per CU, 4 rows at least a group
+    // 28 waves per CU, 4 rows at least a group
     p.least_rows = 4;
-    const int64_t pieces = pieces_of(d, dtype), x = group_threads(pieces), held = (int64_t)8192 * 64 / ((pieces + x - 1) / x * x);
+    const int64_t pieces = pieces_of(d, dtype), x = group_threads(pieces), held = (int64_t)7168 * 64 / ((pieces + x - 1) / x * x);
     const int64_t wanted = (positions + p.least_rows - 1) / p.least_rows;
     p.stretches = wanted < held ? wanted : held < 64 ? 64 : held;
     if (p.stretches > wanted) p.stretches = wanted;
@@ -623,6 +660,7 @@ void launch_embedding_bwd(const EmbeddingArgs& a, const EmbeddingPlan& p, void* 
     u.key = s.key_out; u.pos = s.pos_out; u.counts = s.counts; u.stretches = p.stretches; u.least_rows = p.least_rows;
     u.pieces = pieces_of(a.d, a.dtype);
     u.part = (float*)(w + p.part); u.flags = (uint8_t*)s.flags; u.d = a.d; u.scale = a.scale;
+    u.once = a.positions * a.d * (a.dtype == RAPID_DTYPE_BF16 ? 2 : 4) > BEYOND_CACHES;
     auto go = [&](auto* out) {
         if (a.dtype == RAPID_DTYPE_BF16) sum_d<BF16x8>(u, a.V, dh, out, st);
         else if (a.d % 4 == 0) sum_d<F32x4>(u, a.V, dh, out, st);

@@ -26,6 +26,21 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const T* __restrict_
     if (bad && dev_status) atomicOr(dev_status, RAPID_STATUS_NONFINITE_VALUE);
 }
 
+// rows that do not begin on 16 bytes
+__device__ __forceinline__ Raw8<bf16_t> load8_any(const bf16_t* row, int64_t c, int64_t n) {
+    uint32_t w[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        w[e] = (c + 2 * e < n ? (uint32_t)row[c + 2 * e] : 0u) | (c + 2 * e + 1 < n ? (uint32_t)row[c + 2 * e + 1] << 16 : 0u);
+    return Raw8<bf16_t>{make_uint4(w[0], w[1], w[2], w[3])};
+}
+__device__ __forceinline__ Raw8<float> load8_any(const float* row, int64_t c, int64_t n) {
+    float f[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = c + e < n ? row[c + e] : 0.f;
+    return Raw8<float>{make_float4(f[0], f[1], f[2], f[3]), make_float4(f[4], f[5], f[6], f[7])};
+}
+
 // W stored [d, V]: a block takes the 128 rows of one block index and 128 columns.  A thread holds 8 x 8 elements (rows 8 (tid / 16) on, columns
 // 8 (tid % 16) on); the columns' largest magnitudes meet in the LDS, and so do the rounded values, which leave as whole 128-byte rows.
 template <class T, bool WHOLE>
@@ -37,29 +52,35 @@ __global__ __launch_bounds__(256) void quantize_columns_kernel(const T* __restri
     const int64_t v0 = (int64_t)blockIdx.x * 128, b = blockIdx.y, k0 = b * FP8_BLOCK;
     const int tc = threadIdx.x & 15, tr = threadIdx.x >> 4;
     const int64_t c = v0 + tc * 8;
-    float x[8][8];
+    Raw8<T> x[8];                   // as stored: half the registers of floats
 #pragma unroll
     for (int r = 0; r < 8; ++r) {
         const int64_t k = k0 + tr * 8 + r;
-        if (WHOLE) {
-            if (k < d && c < V) load8(W + k * V, c, V, x[r]);
-            else
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[r][e] = 0.f;
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[r][e] = k < d && c + e < V ? to_float(W[k * V + c + e]) : 0.f;
-        }
+        x[r].clear();
+        if (k >= d) continue;
+        if (WHOLE) x[r] = load8(W + k * V, c, V);
+        else x[r] = load8_any(W + k * V, c, V);
     }
+    uint32_t top = 0u;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         uint32_t most = 0u;
 #pragma unroll
-        for (int r = 0; r < 8; ++r) most = max(most, finite_magnitude(x[r][e]));
+        for (int r = 0; r < 8; ++r) most = max(most, magnitude(x[r][e]));
         s_most[tr][tc * 8 + e] = most;
+        top = max(top, most);
+    }
+    const bool bad = top >= INFINITY_BITS;
+    if (bad) {                      // rare: the largest finite ones instead
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            uint32_t most = 0u;
+#pragma unroll
+            for (int r = 0; r < 8; ++r) most = max(most, finite_magnitude(x[r][e]));
+            s_most[tr][tc * 8 + e] = most;
+        }
     }
     __syncthreads();
-    bool bad = false;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         uint32_t most = 0u;
@@ -67,9 +88,13 @@ __global__ __launch_bounds__(256) void quantize_columns_kernel(const T* __restri
         for (int g = 0; g < 16; ++g) most = max(most, s_most[g][tc * 8 + e]);
         const uint32_t s = block_scale(most);
         const float inv = scale_inverse(s);
+        float f[8];
 #pragma unroll
-        for (int r = 0; r < 8; ++r) x[r][e] = not_finite_is_nan(x[r][e], bad);
-        s_out[tc * 8 + e][tr] = make_uint2(to_fp8x4(x[0][e], x[1][e], x[2][e], x[3][e], inv), to_fp8x4(x[4][e], x[5][e], x[6][e], x[7][e], inv));
+        for (int r = 0; r < 8; ++r) f[r] = x[r][e];
+        if (bad)
+#pragma unroll
+            for (int r = 0; r < 8; ++r) f[r] = not_finite_is_nan(f[r]);
+        s_out[tc * 8 + e][tr] = make_uint2(to_fp8x4(f[0], f[1], f[2], f[3], inv), to_fp8x4(f[4], f[5], f[6], f[7], inv));
         if (tr == 0 && c + e < V) scales[(c + e) * scale_row + b] = (uint8_t)s;
     }
     // the bytes that fill a row of scales up to whole words
