@@ -305,15 +305,16 @@ __device__ __forceinline__ void pin(f32x16 (&acc)[S::WI][S::WJ]) {
 // A memory instruction holds its wave until the pipeline takes it, so the requests are spread over the MFMAs.  Requests are buffer loads (scalar base and
 // offset, one register per lane): with 64-bit lane addresses the kernel spilled.
 // 16384 x 1536 on 151936: 3.00 ms = 2.54 PFLOP/s (one step at a time, as below: 3.25); the MFMAs alone 2.08 ms at the clock that the power limit leaves
-// them, the epilogue adds 0.23, the LDS reads 0.3, the requests 0.4.  4 waves of 128 x 128: 3.31 (a third fewer LDS reads, but nobody
+// them, the epilogue adds 0.23, the LDS reads 0.3, the requests 0.4.  TAIL: waves without a live token row leave the products out (290 rows: 105 -> 92 us; more
+// row tiles hardly notice, and pay 1.5 %).  4 waves of 128 x 128: 3.31 (a third fewer LDS reads, but nobody
 // to fill a wave's gaps).
-template <class S>
+template <class S, bool TAIL>
 __global__ __launch_bounds__(S::NT, 1) void fwd_fp8_kernel(Fp8FwdArgs a) {
     constexpr int WI = S::WI, WJ = S::WJ, B_STAGE = S::BI * 128, STAGE = (S::BI + S::BJ) * 128, SC = 2 * STAGE, SCB = (S::BI + S::BJ) * 4;
     constexpr int NA = S::BI / (8 * S::NW), NB = S::BJ / (8 * S::NW), T = NA + NB;
     constexpr int NS = (S::BI + S::BJ) / (64 * S::NW);      // scale requests of a wave: rows 64 (wave + n NW) ..
     extern __shared__ __attribute__((aligned(128))) char lds[];
-    const int Mr = a.counts[CNT_MR];
+    const int Mr = a.counts[CNT_MR], M = a.counts[CNT_M];
     if (a.row0 >= Mr) return;
     const int tilesM = min(a.tilesM * (256 / S::BJ), (int)((Mr - a.row0 + S::BJ - 1) / S::BJ));
     const int per = ids_for(a.tilesV, tilesM) / 8, wgs = gridDim.x / 8, x = blockIdx.x & 7, w = blockIdx.x >> 3;
@@ -321,10 +322,13 @@ __global__ __launch_bounds__(S::NT, 1) void fwd_fp8_kernel(Fp8FwdArgs a) {
     const int steps = (int)(row / FP8_BLOCK);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wave_i = wave % S::NWI, wave_j = wave / S::NWI;
+    // TAIL: where a round of workgroups covers whole groups of the order, a workgroup would meet the same (maybe cheap) row tile in every round: it
+    // moves on by one row tile per round then
+    const int turn = TAIL && wgs % (a.gi * tilesM) == 0 ? a.gi : 0;
     auto tile = [&](int r) {
-        const int pos = r * wgs + w;
+        const int pos = r * wgs + (w + r * turn) % wgs;
         TileId t = tile_of_vid(x * per + pos, a.tilesV, tilesM, a.gi);
-        t.valid = __builtin_amdgcn_readfirstlane(t.valid && pos < per);
+        t.valid = __builtin_amdgcn_readfirstlane(t.valid && r * wgs < per && pos < per);
         t.ti = __builtin_amdgcn_readfirstlane(t.ti);
         t.tj = __builtin_amdgcn_readfirstlane(t.tj);
         return t;
@@ -389,6 +393,7 @@ __global__ __launch_bounds__(S::NT, 1) void fwd_fp8_kernel(Fp8FwdArgs a) {
     for (int r = 0; t.valid; ++r) {
         const TileId next = tile(r + 1);
         const At pn = next.valid ? point(next) : p;      // none is left: this tile's first steps again, into idle stages
+        const bool live = !TAIL || a.row0 + (int64_t)t.tj * S::BJ + wave_j * (WJ * 32) < M;
         f32x16 acc[WI][WJ];
 #pragma unroll
         for (int ib = 0; ib < WI; ++ib)
@@ -406,7 +411,7 @@ __global__ __launch_bounds__(S::NT, 1) void fwd_fp8_kernel(Fp8FwdArgs a) {
             read_frag(fa, at_a + cur, 1);
             read_frag(fb, at_a + to_b + cur, 1);
             fence();
-            mma_half_asking<S, 0>(a0, b0, sa, sb, acc, [](int) {});
+            if (live) mma_half_asking<S, 0>(a0, b0, sa, sb, acc, [](int) {});
             pin<S>(acc);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             take(a1, fa); take(b1, fb);
@@ -426,7 +431,12 @@ __global__ __launch_bounds__(S::NT, 1) void fwd_fp8_kernel(Fp8FwdArgs a) {
             read_bytes(na, at_sa + rbuf + (k1 & 3));
             read_bytes(nb, at_sa + to_sb + rbuf + (k1 & 3));
             fence();
-            mma_half_asking<S, T>(a1, b1, sa, sb, acc, [&](int q) { ask(qa, qb, q, lds + cur); });
+            if (live) {
+                mma_half_asking<S, T>(a1, b1, sa, sb, acc, [&](int q) { ask(qa, qb, q, lds + cur); });
+            } else {
+#pragma unroll
+                for (int q = 0; q < T; ++q) ask(qa, qb, q, lds + cur);
+            }
             fence();
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             take(a0, fa); take(b0, fb);
@@ -436,7 +446,7 @@ __global__ __launch_bounds__(S::NT, 1) void fwd_fp8_kernel(Fp8FwdArgs a) {
             pin<S>(acc);
             cur = nxt;
         }
-        epilogue_fp8<S>(a, t, first_v(t), a.row0 + (int64_t)t.tj * S::BJ, acc);
+        if (live) epilogue_fp8<S>(a, t, first_v(t), a.row0 + (int64_t)t.tj * S::BJ, acc);
         t = next;
         p = pn;
     }
@@ -614,11 +624,11 @@ void launch_small(const Fp8FwdArgs& a, hipStream_t st) {
     allow_lds<&fwd_fp8_small_kernel<S>>(stages);
     fwd_fp8_small_kernel<S><<<tile_grid<S>(a), S::NT, stages, st>>>(a);
 }
-template <class S>
+template <class S, bool TAIL>
 void launch_tiles(const Fp8FwdArgs& a, hipStream_t st) {
     constexpr int bytes = 2 * (S::BI + S::BJ) * (128 + 4);
-    allow_lds<&fwd_fp8_kernel<S>>(bytes);
-    fwd_fp8_kernel<S><<<tile_grid<S>(a), S::NT, bytes, st>>>(a);
+    allow_lds<&fwd_fp8_kernel<S, TAIL>>(bytes);
+    fwd_fp8_kernel<S, TAIL><<<tile_grid<S>(a), S::NT, bytes, st>>>(a);
 }
 template <class F>
 void launch_few(const Fp8FwdArgs& a, int slots, hipStream_t st) {
@@ -648,7 +658,7 @@ void launch_fwd_fp8(const Fp8FwdArgs& a, const Fp8Way& p, hipStream_t st) {
     case FP8_SMALL_HEAD: launch_small<Tiles>(a, st); break;
     case FP8_32_ROWS: launch_few<Few<1, 7>>(a, p.slots, st); break;
     case FP8_64_ROWS: launch_few<Few<2, 6>>(a, p.slots, st); break;
-    case FP8_TILES: launch_tiles<Tiles>(a, st); break;
+    case FP8_TILES: a.tilesM <= 4 ? launch_tiles<Tiles, true>(a, st) : launch_tiles<Tiles, false>(a, st); break;
     }
 }
 
