@@ -134,3 +134,33 @@ def small_spec(name="small", dtype="bf16", d=128, V=1000, prompts=4, G=4, len_lo
                sigma=0.01, reward="bernoulli", **kw):
     """Reduced-size spec with the same recipe, for parity tests the oracle finishes in seconds."""
     return WorkloadSpec(name, dtype, d, V, prompts, G, len_lo, len_hi, sigma, reward, **kw)
+
+
+def make_tied_workload(spec: WorkloadSpec, seed: int = 0, device: str = "cpu", scale: float = 1.0, as_served=None):
+    """Generations of the smallest policy with a tied table E [V,d]: the hidden state at a position is scale * E[x] with x the token
+    before it (the first one: the prompt's), the logits are hidden . E.  as_served(rows [R,d]) -> fp32: the rows as the policy that
+    draws the tokens multiplies them (None: as they are stored), e.g. after a pass through 8 bits.
+    Returns a dict of tensors on `device`: table [V,d], inputs [N,T] int32 (x), tokens, mask, rewards, group_ids, lengths; plus K, scale, spec."""
+    dev = torch.device(device)
+    gen = torch.Generator(device=dev)
+    gen.manual_seed(seed)
+    as_served = as_served or (lambda rows: rows.float())
+    N, T, d, V = spec.N, spec.T, spec.d, spec.V
+    lengths = torch.randint(spec.len_lo, spec.len_hi + 1, (N,), generator=gen, device=dev)
+    mask = (torch.arange(T, device=dev)[None, :] < lengths[:, None]).to(torch.uint8)
+    # a row's product with itself, the logit of drawing a token again, is about 2
+    table = (torch.randn((V, d), generator=gen, device=dev) * math.sqrt(2.0 / (scale * d))).to(_torch_dtype(spec.dtype))
+    head = as_served(table)
+    prompts = torch.randint(0, V, (spec.prompts,), generator=gen, device=dev)
+    x = prompts.repeat_interleave(spec.G)
+    inputs, tokens = (torch.zeros((N, T), dtype=torch.int32, device=dev) for _ in range(2))
+    for t in range(T):
+        z = as_served((table[x].float() * scale).to(table.dtype)) @ head.t()
+        u = torch.rand(z.shape, generator=gen, device=dev)
+        y = (z - torch.log(-torch.log(u.clamp_min(1e-30)).clamp_min(1e-30))).argmax(dim=1)
+        inputs[:, t], tokens[:, t] = x.to(torch.int32), y.to(torch.int32)
+        x = y
+    rewards = (torch.rand((N,), generator=gen, device=dev) < spec.reward_p).float()
+    group_ids = (torch.arange(N, device=dev) // spec.G).to(torch.int32)
+    return dict(spec=spec, table=table, inputs=inputs, tokens=tokens * mask.to(torch.int32), mask=mask, rewards=rewards,
+                group_ids=group_ids, lengths=lengths, K=spec.prompts, scale=scale)

@@ -259,7 +259,9 @@ LOGP = [  # dtype, N, T, d, V, mask, temperature
     ("bf16", 5, 13, 264, 70, "ragged", 1.0), ("bf16", 1, 129, 384, 400, "none", 1.0), ("bf16", 3, 300, 200, 700, "holes", 0.5), ("bf16", 9, 1000, 64, 130, "ragged", 1.0),
     ("bf16", 2, 4200, 72, 300, "holes", 1.0), ("bf16", 1, 17000, 16, 90, "none", 1.0),
     ("f32", 1, 1, 1, 2, "none", 1.0), ("f32", 8, 1, 1001, 600, "none", 1.0), ("f32", 6, 33, 127, 259, "holes", 1.0), ("f32", 2, 70, 515, 1300, "ragged", 0.9),
-    ("f32", 1, 257, 2049, 300, "none", 1.0),
+    ("f32", 1, 257, 2049, 300, "none", 1.0), ("bf16", 32, 1, 136, 256, "none", 1.0), ("bf16", 33, 1, 136, 256, "none", 1.0), ("bf16", 8, 8, 264, 385, "holes", 1.0),
+    ("bf16", 5, 13, 264, 384, "ragged", 1.0), ("bf16", 4, 250, 520, 3001, "holes", 1.0), ("bf16", 17, 1000, 136, 300, "ragged", 1.0), ("f32", 2, 16, 4500, 1031, "none", 1.0),
+    ("bf16", 1, 1100, 256, 5000, "holes", 1.0),
 ]
 
 
@@ -422,3 +424,68 @@ def test_graphs_that_share_a_workspace(rb):
             _run_calls(rb, s, ws)
             torch.cuda.synchronize()
             assert all(torch.equal(a, b) for a, b in zip(got, _results(s))), (turn, z)
+
+
+# ------------------------------------------------------------------------------------------- one update of a tied table
+def _tied(rb, dtype, **kw):
+    from paper_2510_03515_amd import iw_grpg as ig
+    from paper_2510_03515_amd import workloads as wl
+    spec = wl.small_spec("tied", dtype, **dict(dict(d=72, V=301, prompts=4, G=4, len_lo=2, len_hi=21, reward="bernoulli"), **kw))
+    return ig, wl.make_tied_workload(spec, seed=3, device="cuda", scale=spec.d ** 0.5, as_served=ig.served_in_8_bits)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_tied_step_against_the_formula_and_differences(rb, dtype):
+    """The table's gradient of one loss step through both uses: against the loss oracle's dHidden and dW, put together by the table oracle, and (fp32) against
+    central differences of the objective, in float64, along random directions."""
+    from oracle import rapid_oracle as loss_orc
+    ig, w = _tied(rb, dtype)
+    E, scale, N = w["table"], float(np.float32(w["scale"])), w["tokens"].shape[0]
+    inputs, tokens, mask = w["inputs"], w["tokens"], w["mask"]
+    hidden = rb.rapid_embedding_fwd(E, inputs, mask, scale=scale)
+    W8 = rb.rapid_quantize_fp8(E, w_layout=rb.W_VD)
+    logp_b, _ = rb.rapid_logprob_fwd_fp8(hidden, W8, tokens, mask)
+    out = rb.rapid_iw_pg_loss_fwd_bwd(hidden, E, tokens, mask, logp_b, w["rewards"], w["group_ids"], w["K"], w_layout=rb.W_VD)
+    head = out.dW.clone()
+    rb.rapid_embedding_bwd(out.dhidden, inputs, mask, E.shape[0], scale=scale, dtable=out.dW, accumulate=True)
+    # the lookup's share, from the states' gradient as the loss step returned it
+    ref, size, terms = orc.embedding_bwd(_f64(out.dhidden), inputs.cpu().numpy(), mask.cpu().numpy(), E.shape[0], scale)
+    _check_gradient(out.dW, head, ref, size, terms, "f32")
+    # all of it, from the definition; the loss step's own bounds (1e-5 of a tensor in fp32, 2e-2 in bf16) hold for the sum of its two parts
+    h64, E64 = _f64(hidden), _f64(E)
+    want = loss_orc.iw_pg_loss_fwd_bwd(h64, E64.T.copy(), tokens.cpu().numpy(), mask.cpu().numpy(), _f64(logp_b), _f64(w["rewards"]), w["group_ids"].cpu().numpy(), w["K"])
+    both = want["dW"].T + orc.embedding_bwd(want["dH"], inputs.cpu().numpy(), mask.cpu().numpy(), E.shape[0], scale)[0]
+    parts = np.linalg.norm(want["dW"]) + np.linalg.norm(both - want["dW"].T)
+    assert np.linalg.norm(_f64(out.dW) - both) <= (1e-5 if dtype == "f32" else 2e-2) * parts
+    if dtype != "f32":
+        return
+    m, x, y, adv = mask.cpu().numpy(), inputs.cpu().numpy(), tokens.cpu().numpy(), np.asarray(want["adv"])
+
+    def objective(table):       # advantages held: the gradient acts on the ratios alone
+        total = 0.0
+        for n in range(N):
+            at = np.nonzero(m[n])[0]
+            z = scale * table[x[n, at]] @ table.T
+            lp = z[np.arange(len(at)), y[n, at]] - np.log(np.exp(z - z.max(axis=1, keepdims=True)).sum(axis=1)) - z.max(axis=1)
+            total -= np.exp(np.sum(lp - _f64(logp_b)[n, at])) * adv[n] / N
+        return total
+
+    rng = np.random.default_rng(1)
+    for _ in range(4):
+        along = rng.standard_normal(E64.shape)
+        along /= np.linalg.norm(along)
+        step = 1e-5                                  # truncation ~ step^2, cancellation 2^-53 / step: 1e-10 each, far below 1e-5 of the gradient
+        slope = (objective(E64 + step * along) - objective(E64 - step * along)) / (2 * step)
+        assert abs(slope - np.sum(_f64(out.dW) * along)) <= 1e-5 * parts + 1e-8
+
+
+@pytest.mark.parametrize("optimizer,cache", [("sgd", False), ("adamw", True)])
+def test_tied_inner_loop_runs(rb, optimizer, cache):
+    """The command's path: every step's calls together, and a behaviour policy in 8 bits that is close to, and not, the table's own."""
+    ig, w = _tied(rb, "bf16", d=136, V=700, prompts=8)
+    before = w["table"].clone()
+    log, summary, E = ig.iw_grpg_tied(w, inner_steps=4, lr=2e-4 if optimizer == "sgd" else 2e-6, optimizer=optimizer, logits_cache=cache)
+    assert len(log) == 4 and all(np.isfinite(list(r.values())).all() for r in log)
+    assert 0.0 < log[0]["max_abs_s"] < 1.0
+    assert np.isfinite(summary["reward_final_is_estimate"]) and abs(summary["reward_behaviour"] - w["rewards"].mean().item()) < 1e-5
+    assert torch.equal(w["table"], before) and not torch.equal(E, before) and torch.isfinite(E.float()).all()
