@@ -176,6 +176,18 @@ def _shape(t, shape, name):
         raise TypeError(f"{name}: shape {tuple(t.shape)}, need {tuple(shape)}")
 
 
+def _here(tensors, dev_status, workspace=None):
+    """The library works on the current device's current stream, sets bits of one int32 and takes workspaces by their bytes."""
+    if dev_status is not None:
+        _need(dev_status, torch.int32, "dev_status"); _shape(dev_status.view(-1)[:1], (1,), "dev_status")
+    if workspace is not None:
+        _need(workspace, torch.uint8, "workspace")
+    dev = torch.cuda.current_device()
+    for t in (*tensors, dev_status, workspace):
+        if t is not None and t.get_device() != dev:
+            raise TypeError(f"a tensor lies on {t.device}, the current device is {dev}")
+
+
 def rapid_version():
     return load().rapid_version()
 
@@ -313,6 +325,7 @@ def rapid_embedding_fwd(table, tokens, mask=None, scale=1.0, out=None, dev_statu
     if out is None:
         out = torch.empty((N, T, d), dtype=table.dtype, device=table.device)
     _need(out, table.dtype, "out"); _shape(out, (N, T, d), "out")
+    _here((table, tokens, mask, out), dev_status)
     _check(load().rapid_embedding_fwd(_ptr(table), _ptr(tokens), _ptr(mask), N, T, d, V, _dtype_code(table), float(scale),
                                       _ptr(out), _ptr(dev_status), _stream()))
     return out
@@ -334,6 +347,7 @@ def rapid_embedding_bwd(dhidden, tokens, mask, V, scale=1.0, dtable=None, dw_dty
     _need(dtable, dtable.dtype, "dtable"); _shape(dtable, (V, d), "dtable")
     if workspace is None:
         workspace = alloc_workspace(rapid_workspace_bytes(OP_EMBEDDING_BWD, N, T, d, V, 1, dt), dhidden.device)
+    _here((dhidden, tokens, mask, dtable), dev_status, workspace)
     _check(load().rapid_embedding_bwd(_ptr(dhidden), _ptr(tokens), _ptr(mask), N, T, d, V, dt, float(scale),
                                       _dtype_code(dtable), int(bool(accumulate)), _ptr(dtable), _ptr(dev_status),
                                       _ptr(workspace), workspace.numel(), _stream()))
@@ -362,6 +376,7 @@ def rapid_quantize_fp8(W, w_layout=W_DV, out=None, dev_status=None):
                         torch.empty((V, lib.rapid_fp8_scale_bytes(d)), dtype=torch.uint8, device=W.device), d)
     if out.d != d or out.values.shape[0] != V:
         raise TypeError("out: another head's size")
+    _here((W, out.values, out.scales), dev_status)
     _check(load().rapid_quantize_fp8(_ptr(W), d, V, _dtype_code(W), w_layout, _ptr(out.values), _ptr(out.scales),
                                      _ptr(dev_status), _stream()))
     return out
@@ -379,6 +394,7 @@ def rapid_logprob_fwd_fp8(hidden, W8, tokens, mask, temperature=1.0, want_lse=Fa
     _need(mask, torch.uint8, "mask"); _shape(mask, (N, T), "mask")
     if workspace is None:
         workspace = alloc_workspace(rapid_workspace_bytes(OP_LOGPROB_FWD_FP8, N, T, d, V, 1, dt), hidden.device)
+    _here((hidden, W8.values, W8.scales, tokens, mask), dev_status, workspace)
     logp = torch.empty((N, T), dtype=torch.float32, device=hidden.device)
     lse = torch.empty((N, T), dtype=torch.float32, device=hidden.device) if want_lse else None
     _check(load().rapid_logprob_fwd_fp8(_ptr(hidden), _ptr(W8.values), _ptr(W8.scales), _ptr(tokens), _ptr(mask), N, T, d, V, dt,

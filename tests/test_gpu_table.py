@@ -489,3 +489,38 @@ def test_tied_inner_loop_runs(rb, optimizer, cache):
     assert 0.0 < log[0]["max_abs_s"] < 1.0
     assert np.isfinite(summary["reward_final_is_estimate"]) and abs(summary["reward_behaviour"] - w["rewards"].mean().item()) < 1e-5
     assert torch.equal(w["table"], before) and not torch.equal(E, before) and torch.isfinite(E.float()).all()
+
+
+def test_another_current_device_is_refused(rb, monkeypatch):
+    """Every call looks where its tensors lie; nothing is launched."""
+    s = _calls(rb, torch.Generator().manual_seed(2), 2, 5, 8, 9)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    calls = [lambda **kw: rb.rapid_embedding_fwd(s["table"], s["tokens"], s["mask"], **kw), lambda **kw: rb.rapid_embedding_bwd(s["dh"], s["tokens"], s["mask"], 9, **kw),
+             lambda **kw: rb.rapid_quantize_fp8(s["table"], w_layout=rb.W_VD, **kw),
+             lambda **kw: rb.rapid_logprob_fwd_fp8(s["hidden"], s["W8"], s["tokens"], s["mask"], **kw)]
+    for call in calls:
+        for word in (status.cpu(), status.float(), status[:0]):
+            with pytest.raises(TypeError):
+                call(dev_status=word)
+        call(dev_status=status)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: torch.cuda.device_count())
+    for call in calls:
+        with pytest.raises(TypeError, match="current device"):
+            call(dev_status=status)
+
+
+@pytest.mark.parametrize("key,values", [(10, (0, 1, 3, 8, 1024)), (13, (1, 2))])
+def test_logprob_tile_order_changes_nothing(rb, key, values):
+    """The order of the 8-bit logits' tiles and the row tiles of a launch: the same bits."""
+    gen = torch.Generator().manual_seed(21)
+    N, T, d, V = 4, 290, 264, 70001
+    W8 = rb.rapid_quantize_fp8(_head(V, d, gen, "bf16").cuda(), w_layout=rb.W_VD)
+    hidden, tokens, m = torch.randn((N, T, d), generator=gen).bfloat16().cuda(), _ids("zipf", N, T, V, gen).cuda(), _mask("holes", N, T, gen).cuda()
+    want, want_lse = rb.rapid_logprob_fwd_fp8(hidden, W8, tokens, m, want_lse=True)
+    try:
+        for value in values:
+            assert rb.load().rapid_set_tuning(key, value) == 0
+            p, s = rb.rapid_logprob_fwd_fp8(hidden, W8, tokens, m, want_lse=True)
+            assert torch.equal(p, want) and torch.equal(s, want_lse), value
+    finally:
+        rb.load().rapid_set_tuning(key, {10: 4, 13: 64}[key])

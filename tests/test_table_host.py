@@ -146,3 +146,20 @@ def test_binding_refuses_cpu_tensors_and_shapes(rb):
         rb.rapid_embedding_bwd(torch.zeros(2, 3, 8), tokens, None, 5)
     with pytest.raises(TypeError):
         rb.Fp8Weight(torch.zeros(5, 128), torch.zeros(5, 4, dtype=torch.uint8), 8)
+
+
+def test_binding_refuses_other_devices_status_words_and_workspaces(rb, monkeypatch):
+    """What every one of the calls checks last, with tensors that only claim to lie on a GPU."""
+    class On:
+        def __init__(self, device, dtype=torch.int32, n=1, contiguous=True):
+            self.device, self.dtype, self.n, self.is_cuda, self.contiguous = f"cuda:{device}", dtype, n, device >= 0, contiguous
+        def get_device(self): return int(self.device[5:])
+        def is_contiguous(self): return self.contiguous
+        def view(self, *_): return torch.zeros(self.n)
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    rb._here((On(1), None), None)
+    rb._here((On(1),), On(1), On(1, torch.uint8, 4096))
+    for args in (((On(0),), None), ((On(1), On(2)), None), ((On(1),), On(0)), ((On(1),), On(-1)), ((On(1),), On(1, torch.uint8)), ((On(1),), On(1, n=0)),
+                 ((On(1),), None, On(0, torch.uint8)), ((On(1),), None, On(1, torch.float32)), ((On(1),), None, On(1, torch.uint8, contiguous=False))):
+        with pytest.raises(TypeError):
+            rb._here(*args)
