@@ -25,10 +25,10 @@ extern "C" {
  *        with 8 and 16; the sums of dHidden and dW are taken in another order: they differ by the fp32 rounding of the
  *        accumulators.  Workspace sizes follow the tiles: set it before asking for them.
  * keys 10, 11, 12: tile-order blocking (tiles along the first tile dimension that share one tile of
- *        the second before the order moves on) of the logits kernels, the dHidden kernel (0 = all)
+ *        the second before the order moves on) of the logits kernels (the 8-bit one among them), the dHidden kernel (0 = all)
  *        and the dW kernel; defaults 4, 0, 2 were measured best on MI355X.  Results are identical.
  * key 13: token-row tiles (of 256 rows) per launch of the two logits kernels (forward and dz),
- *        default 64: they sweep all of W over one such block of rows at a time so that the block's
+ *        default 64 (also of the 8-bit logits kernel): they sweep all of W over one such block of rows at a time so that the block's
  *        hidden rows stay in the memory-side cache.  Results are identical.
  * key 14: 1 (default) / 0: the dHidden kernel reads W from a tile-blocked copy (one contiguous
  *        32 KiB block per 256-row tile and 64-column step) / from the row-major copy.  Results

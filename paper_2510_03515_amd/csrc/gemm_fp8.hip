@@ -645,7 +645,7 @@ int stream_slots(int64_t V) {
 
 }  // namespace
 
-// 16 rows, d 1536, V 151936: tiles 65 us, the head read at 3.6 TB/s; few rows 36.7 us, 6.4 TB/s.  60 rows: 65 and 38.6 us.
+// 16 rows, d 1536, V 151936: tiles 65 us, few rows 37 (43 with nothing of the head in the memory-side cache: 5.4 TB/s); 60 rows 65 and 39.
 Fp8Way fp8_way(int64_t positions, int64_t d, int64_t V) {
     if (V >= Tiles::BI && d > FP8_BLOCK && positions <= 64) return Fp8Way{positions <= 32 ? FP8_32_ROWS : FP8_64_ROWS, stream_slots(V)};
     return Fp8Way{V >= Tiles::BI && d > FP8_BLOCK ? FP8_TILES : FP8_SMALL_HEAD, 2 * (int)((V + 255) / 256)};
