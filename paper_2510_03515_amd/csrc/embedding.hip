@@ -485,17 +485,39 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(SumArgs a, const typ
     }
 }
 
-// Joins the sums that crossed ends of stretches: the block of the stretch in which such an id began adds up what the stretches after it left, in
-// order (in MERGE_WAVES consecutive shares, then these in order).  The blocks behind those of the stretches clear the rows of the ids that do
-// not occur, ZERO_ROWS of them a wave.
-constexpr int MERGE_WAVES = 8, ZERO_ROWS = 16;
+// acc += what stretches from .. to - 1 left of the id whose run ends in stretch `last`, in order; U of them under way together, the last ones too
+template <int U, int N>
+__device__ __forceinline__ void add_parts(const float* __restrict__ part, int64_t d, int64_t from, int64_t to, int64_t last, float (&acc)[N]) {
+    for (int64_t c0 = from; c0 < to; c0 += U) {
+        float v[U][N];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int64_t c = min(c0 + u, to - 1);
+            const float* q = part + (c * 2 + (c == last ? 0 : 1)) * d;
+#pragma unroll
+            for (int e = 0; e < N; ++e) v[u][e] = q[e];
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int e = 0; e < N; ++e) acc[e] += c0 + u < to ? v[u][e] : 0.f;
+    }
+}
+// Joins the sums that crossed ends of stretches, and clears the rows of the ids that do not occur.  A wave looks at one stretch, and for the id that begins
+// in it and goes on behind it adds up what the stretches after it left, 64 pieces of the columns; ids of more than SHORT_RUN stretches are left to the
+// block's waves together (in MERGE_WAVES consecutive shares, then these in order).  The blocks behind those clear ZERO_ROWS ids a wave.
+// (A block a stretch: 6144 blocks of little more than two trips to the keys each, 8.6 of 36 us in the bandit's batch.)
+constexpr int MERGE_WAVES = 8, ZERO_ROWS = 16, SHORT_RUN = 16;
 template <class P, class D, bool ACC, class W>
 __global__ __launch_bounds__(64 * MERGE_WAVES) void embedding_merge_kernel(SumArgs a, D* __restrict__ dE, int64_t V, int64_t row_words) {
     __shared__ float s_sum[MERGE_WAVES][64][P::N];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t s = blockIdx.x;
-    if (!ACC && s >= a.stretches - 1) {
-        const int64_t v0 = ((s - (a.stretches - 1)) * MERGE_WAVES + wave) * ZERO_ROWS;
+    __shared__ int64_t s_last[MERGE_WAVES];                 // of the wave's run, if all waves are to join it
+    __shared__ int s_key[MERGE_WAVES];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int chunks = (a.pieces + 63) / 64;                // of a row: a block each
+    const int64_t joins = (a.stretches + MERGE_WAVES - 1) / MERGE_WAVES * chunks;
+    if (!ACC && blockIdx.x >= joins) {
+        const int64_t v0 = ((blockIdx.x - joins) * MERGE_WAVES + wave) * ZERO_ROWS;
         unsigned long long rows = __ballot(lane < ZERO_ROWS && v0 + lane < V && a.flags[v0 + lane] == 0);
         for (; rows; rows &= rows - 1) {
             W* row = (W*)dE + (v0 + __ffsll((long long)rows) - 1) * row_words;
@@ -503,44 +525,62 @@ __global__ __launch_bounds__(64 * MERGE_WAVES) void embedding_merge_kernel(SumAr
         }
         return;
     }
+    const int64_t s0 = blockIdx.x / chunks * (int64_t)MERGE_WAVES, s = s0 + wave;
+    const int piece = (int)(blockIdx.x % chunks) * 64 + lane;
     const int64_t M = a.counts[0], n_rows = stretch_rows(a, M), begin = s * n_rows, end = begin + n_rows;
-    if (end >= M) return;                                   // nothing goes on behind the last stretch
-    // (the keys are asked for together)
-    const int key = a.key[end - 1], key_behind = a.key[end], key_first = a.key[begin], key_before = a.key[begin > 0 ? begin - 1 : 0];
-    if (key_behind != key) return;
-    if (key_first == key && begin > 0 && key_before == key) return;      // began in an earlier stretch
-    int64_t last = s + 1;                                   // the stretch in which the id's run ends: 64 are looked at together
-    for (;; last += 64) {
-        const int64_t at = (last + lane + 1) * n_rows - 1;
-        const unsigned long long other = __ballot(at >= M - 1 || a.key[at < M ? at : M - 1] != key);
-        if (other) { last += __ffsll((long long)other) - 1; break; }
+    const float* const part = a.part + (int64_t)piece * P::N;
+    auto finish = [&](int key, float (&acc)[P::N]) {
+        D* to_row = dE + (int64_t)key * a.d + (int64_t)piece * P::N;
+        float old[ACC ? P::N : 1];
+        load_row<P, D, ACC>(to_row, old);
+        store_row<P, D, ACC>(to_row, acc, old, a.scale);
+    };
+    int64_t last = s;                                       // the stretch in which the run ends (s: none begins here that goes on)
+    int key = 0;
+    if (end < M) {                                          // (nothing goes on behind the last stretch; the keys are asked for together)
+        key = a.key[end - 1];
+        const int behind = a.key[end], first = a.key[begin], before = a.key[begin > 0 ? begin - 1 : 0];
+        if (behind == key && !(first == key && begin > 0 && before == key)) {
+            // the first stretch behind this one whose last row is not the id's, or not there: 64 are looked at together, every one, or (long
+            // runs) every 64th, then the 64 in between
+            auto ends = [&](int64_t c) { return c * n_rows >= M - n_rows || a.key[(c + 1) * n_rows - 1] != key; };
+            int64_t step = 1;
+            for (last = s + 1;;) {
+                const unsigned long long other = __ballot(ends(last + lane * step));
+                last += (other ? __ffsll((long long)other) - 1 : 64) * step;
+                if (other && step == 1) break;
+                if (other) last -= 63;
+                step = other ? 1 : 64;
+            }
+            if (a.key[last * n_rows] != key) --last;        // it ended with the stretch before (its sum there is in slot 0 all the same)
+        }
     }
-    if (a.key[last * n_rows] != key) --last;                // it ended with the stretch before (its sum there is in slot 0 all the same)
-    const int64_t n = last - s + 1, from = s + n * wave / MERGE_WAVES, to = s + n * (wave + 1) / MERGE_WAVES;
-    for (int piece0 = 0; piece0 < a.pieces; piece0 += 64) {
-        const int piece = piece0 + lane;
+    const bool together = last - s >= SHORT_RUN;
+    if (lane == 0) { s_last[wave] = together ? last : -1; s_key[wave] = key; }
+    if (last > s && !together && piece < a.pieces) {
         float acc[P::N];
 #pragma unroll
         for (int e = 0; e < P::N; ++e) acc[e] = 0.f;
-        if (piece < a.pieces) {
-#pragma unroll 4
-            for (int64_t c = from; c < to; ++c) {
-                const float* p = a.part + (c * 2 + (c == last ? 0 : 1)) * a.d + (int64_t)piece * P::N;
+        add_parts<4, P::N>(part, a.d, s, last + 1, last, acc);
+        finish(key, acc);
+    }
+    __syncthreads();
+    for (int w = 0; w < MERGE_WAVES; ++w) {
+        if (s_last[w] < 0) continue;
+        const int64_t begun = s0 + w, n = s_last[w] - begun + 1;
+        float acc[P::N];
 #pragma unroll
-                for (int e = 0; e < P::N; ++e) acc[e] += p[e];
-            }
-        }
+        for (int e = 0; e < P::N; ++e) acc[e] = 0.f;
+        if (piece < a.pieces) add_parts<8, P::N>(part, a.d, begun + n * wave / MERGE_WAVES, begun + n * (wave + 1) / MERGE_WAVES, s_last[w], acc);
 #pragma unroll
         for (int e = 0; e < P::N; ++e) s_sum[wave][lane][e] = acc[e];
         __syncthreads();
         if (wave == 0 && piece < a.pieces) {
-            for (int w = 1; w < MERGE_WAVES; ++w)
 #pragma unroll
-                for (int e = 0; e < P::N; ++e) acc[e] += s_sum[w][lane][e];
-            D* to_row = dE + (int64_t)key * a.d + (int64_t)piece * P::N;
-            float old[ACC ? P::N : 1];
-            load_row<P, D, ACC>(to_row, old);
-            store_row<P, D, ACC>(to_row, acc, old, a.scale);
+            for (int o = 1; o < MERGE_WAVES; ++o)
+#pragma unroll
+                for (int e = 0; e < P::N; ++e) acc[e] += s_sum[o][lane][e];
+            finish(s_key[w], acc);
         }
         __syncthreads();
     }
@@ -560,8 +600,8 @@ void sum_t(const SumArgs& s, int64_t V, int64_t row_words, const void* dh, D* dE
     const dim3 grid((unsigned)((s.stretches + y - 1) / y), (unsigned)((s.pieces + x - 1) / x)), block(x, y);
     if (x % 64 == 0) embedding_sum_kernel<P, D, ACC, true><<<grid, block, 0, st>>>(s, (const typename P::elem*)dh, dE);
     else embedding_sum_kernel<P, D, ACC, false><<<grid, block, 0, st>>>(s, (const typename P::elem*)dh, dE);
-    const int64_t blocks = s.stretches - 1 + (ACC ? 0 : (V + MERGE_WAVES * ZERO_ROWS - 1) / (MERGE_WAVES * ZERO_ROWS));
-    if (blocks > 0) embedding_merge_kernel<P, D, ACC, W><<<(unsigned)blocks, 64 * MERGE_WAVES, 0, st>>>(s, dE, V, row_words);
+    const int64_t blocks = (s.stretches + MERGE_WAVES - 1) / MERGE_WAVES * ((s.pieces + 63) / 64) + (ACC ? 0 : (V + MERGE_WAVES * ZERO_ROWS - 1) / (MERGE_WAVES * ZERO_ROWS));
+    embedding_merge_kernel<P, D, ACC, W><<<(unsigned)blocks, 64 * MERGE_WAVES, 0, st>>>(s, dE, V, row_words);
 }
 template <class P, class D>
 void sum_d(const SumArgs& s, int64_t V, const void* dh, D* dE, hipStream_t st) {
