@@ -126,7 +126,9 @@ void fwd_t(const EmbeddingArgs& a, const void* table, void* out, hipStream_t st)
 // before: summed from the counts, no scan launch of its own), then every item's rank.  Ranks are found 64 items at a time: ballots over the
 // digit's bits give the lanes that share it, a wave-private count in the LDS the items of earlier rounds.
 // The first pass reads ids and mask in the order of the positions and drops what has no row.
-constexpr int MAX_DIGIT_BITS = 9, MAX_DIGITS = 1 << MAX_DIGIT_BITS;
+// Up to 12 bits are sorted in one pass where there are few blocks, whose counts (16 KB each) every block reads: 512 x 48 positions, V 4096: 13.6 us for
+// 19.2 in two passes of 6 bits, and two launches less.
+constexpr int MAX_DIGIT_BITS = 9, MAX_DIGITS = 1 << MAX_DIGIT_BITS, WIDE_BITS = 12, WIDE_DIGITS = 1 << WIDE_BITS;
 constexpr int SORT_WAVES = 8, SORT_THREADS = 64 * SORT_WAVES;
 
 struct SortPass {
@@ -207,9 +209,10 @@ __device__ __forceinline__ void scan_threads(int v, int* s_sum, int& before, int
     }
 }
 
-template <bool FIRST, int SORT_ITEMS>
+// DIGITS: the most digits of a pass, a multiple of SORT_THREADS
+template <bool FIRST, int SORT_ITEMS, int DIGITS>
 __global__ __launch_bounds__(SORT_THREADS) void sort_count_kernel(SortPass a) {
-    __shared__ int s_hist[MAX_DIGITS];
+    __shared__ int s_hist[DIGITS];
     const int digits = 1 << a.bits;
     for (int i = threadIdx.x; i < digits; i += SORT_THREADS) s_hist[i] = 0;
     if (FIRST) clear_flags(a, (int64_t)blockIdx.x * SORT_THREADS + threadIdx.x, (int64_t)gridDim.x * SORT_THREADS);
@@ -227,53 +230,87 @@ __global__ __launch_bounds__(SORT_THREADS) void sort_count_kernel(SortPass a) {
     for (int i = threadIdx.x; i < digits; i += SORT_THREADS) a.hist[(int64_t)blockIdx.x * digits + i] = s_hist[i];
 }
 
-template <bool FIRST, int SORT_ITEMS>
+template <int DIGITS>
+constexpr int scatter_lds() { return (DIGITS + SORT_WAVES * DIGITS + SORT_WAVES) * 4; }
+template <bool FIRST, int SORT_ITEMS, int DIGITS>
 __global__ __launch_bounds__(SORT_THREADS) void sort_scatter_kernel(SortPass a) {
-    __shared__ int s_base[MAX_DIGITS];                       // where the block's next item of each digit goes
-    __shared__ int s_wave[SORT_WAVES][MAX_DIGITS];           // items of each digit per wave of a round
-    __shared__ int s_sum[SORT_WAVES];
-    const int digits = 1 << a.bits, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    // a thread per digit: items of that digit, and those of them that lie in earlier blocks
-    static_assert(SORT_THREADS >= MAX_DIGITS, "a thread per digit");
-    int total = 0, mine = 0;
-    if (tid < digits) {
-        const int32_t* h = a.hist + tid;
-#pragma unroll 16
+    constexpr int PER = DIGITS / SORT_THREADS;              // digits of a thread, next to each other
+    static_assert(PER * SORT_THREADS == DIGITS, "whole digits a thread");
+    extern __shared__ __attribute__((aligned(16))) char lds[];
+    int* const s_wave = (int*)lds;                           // [SORT_WAVES][digits]: items of each digit per wave of a round
+    int* const s_base = s_wave + SORT_WAVES * DIGITS;        // where the block's next item of each digit goes
+    int* const s_sum = s_base + DIGITS;
+    const int digits = 1 << a.bits, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, d0 = tid * PER;
+    // items of the thread's digits, and those of them that lie in earlier blocks
+    int total[PER], mine[PER], sum = 0;
+#pragma unroll
+    for (int q = 0; q < PER; ++q) total[q] = mine[q] = 0;
+    if (d0 < digits) {
+        const int32_t* h = a.hist + d0;
+#pragma unroll (16 / PER < 4 ? 4 : 16 / PER)
         for (int b = 0; b < a.blocks; ++b) {
-            const int n = h[b << a.bits];
-            total += n;
-            mine += b < (int)blockIdx.x ? n : 0;
+#pragma unroll
+            for (int q = 0; q < PER; ++q) {
+                const int n = h[(b << a.bits) + q];
+                total[q] += n;
+                mine[q] += b < (int)blockIdx.x ? n : 0;
+            }
         }
+#pragma unroll
+        for (int q = 0; q < PER; ++q) sum += total[q];
     }
     int lower, all;
-    scan_threads<SORT_WAVES>(total, s_sum, lower, all);
-    if (tid < digits) s_base[tid] = lower + mine;
+    scan_threads<SORT_WAVES>(sum, s_sum, lower, all);
+    if (d0 < digits) {
+#pragma unroll
+        for (int q = 0; q < PER; ++q) {
+            s_base[d0 + q] = lower + mine[q];
+            lower += total[q];
+        }
+    }
     if (FIRST && blockIdx.x == 0 && tid == 0) a.counts[0] = all;
     const int64_t items = FIRST ? a.items : all;
     const int64_t begin = (int64_t)blockIdx.x * a.tile, end = min(items, begin + a.tile);
     for (int64_t r0 = begin; r0 < end; r0 += SORT_THREADS * SORT_ITEMS) {
         int key[SORT_ITEMS], pos[SORT_ITEMS], rank[SORT_ITEMS];
         sort_keys<FIRST, SORT_ITEMS>(a, r0 + (int64_t)wave * 64 * SORT_ITEMS + lane, 64, end, false, key, pos);
-        for (int i = tid; i < SORT_WAVES * digits; i += SORT_THREADS) s_wave[i >> a.bits][i & (digits - 1)] = 0;
-        __syncthreads();
-#pragma unroll
-        for (int u = 0; u < SORT_ITEMS; ++u) rank[u] = rank_in_wave(key[u], (key[u] >> a.shift) & (digits - 1), a.bits, s_wave[wave]);
-        __syncthreads();
-        if (tid < digits) {                                  // counts -> first places; the base moves on for the next round
-            int at = s_base[tid];
-#pragma unroll
-            for (int w = 0; w < SORT_WAVES; ++w) {
-                const int c = s_wave[w][tid];
-                s_wave[w][tid] = at;
-                at += c;
-            }
-            s_base[tid] = at;
+        if constexpr (PER > 1) {
+            for (int i = tid; i < SORT_WAVES * digits / 4; i += SORT_THREADS) ((int4*)s_wave)[i] = make_int4(0, 0, 0, 0);
+        } else {
+            for (int i = tid; i < SORT_WAVES * digits; i += SORT_THREADS) s_wave[i] = 0;
         }
         __syncthreads();
 #pragma unroll
+        for (int u = 0; u < SORT_ITEMS; ++u) rank[u] = rank_in_wave(key[u], (key[u] >> a.shift) & (digits - 1), a.bits, s_wave + (wave << a.bits));
+        __syncthreads();
+        if constexpr (PER == 1) {       // counts -> first places; the base moves on for the next round
+            if (tid < digits) {
+                int at = s_base[tid];
+#pragma unroll
+                for (int w = 0; w < SORT_WAVES; ++w) {
+                    const int c = s_wave[(w << a.bits) + tid];
+                    s_wave[(w << a.bits) + tid] = at;
+                    at += c;
+                }
+                s_base[tid] = at;
+            }
+            __syncthreads();
+        }
+#pragma unroll
         for (int u = 0; u < SORT_ITEMS; ++u) {
             if (key[u] < 0) continue;
-            const int at = s_wave[wave][(key[u] >> a.shift) & (digits - 1)] + rank[u];
+            const int digit = (key[u] >> a.shift) & (digits - 1);
+            int at = rank[u];
+            if constexpr (PER == 1) {
+                at += s_wave[(wave << a.bits) + digit];
+            } else {                    // more digits than items, and one round: every item adds up the waves before its own
+                at += s_base[digit];
+#pragma unroll
+                for (int w = 0; w < SORT_WAVES - 1; ++w) {
+                    const int c = s_wave[(w << a.bits) + digit];
+                    at += w < wave ? c : 0;
+                }
+            }
             a.key_out[at] = key[u];
             a.pos_out[at] = pos[u];
         }
@@ -616,7 +653,8 @@ int pieces_of(int64_t d, int dtype) { return (int)(d / (dtype == RAPID_DTYPE_BF1
 
 // Items a thread takes in a round of the sort.  Few positions: more blocks with less to do each.
 constexpr int FEW_ITEMS = 2, MANY_ITEMS = 8;
-constexpr int64_t FEW_POSITIONS = 131072, ONE_BLOCK_SORT = 8192;
+constexpr int64_t FEW_POSITIONS = 131072, ONE_BLOCK_SORT = 8192, WIDE_POSITIONS = 32768;
+static_assert(WIDE_POSITIONS <= 256 * SORT_THREADS * FEW_ITEMS, "a block of a wide pass has one round");
 int64_t sort_tile(int64_t positions) {
     const int64_t round = SORT_THREADS * (positions <= FEW_POSITIONS ? FEW_ITEMS : MANY_ITEMS);
     const int64_t per = (positions + 255) / 256;            // at most 256 blocks: every block adds up the counts of all
@@ -627,15 +665,17 @@ void sort_one_t(const SortPass& s, int passes, hipStream_t st) {
     allow_lds<&sort_one_block_kernel<ITEMS>>(one_block_lds<ITEMS>());
     sort_one_block_kernel<ITEMS><<<1, ONE_THREADS, one_block_lds<ITEMS>(), st>>>(s, passes);
 }
-template <int ITEMS>
+template <bool FIRST, int ITEMS, int DIGITS>
 void sort_pass_t(const SortPass& s, hipStream_t st) {
-    if (s.shift == 0) {
-        sort_count_kernel<true, ITEMS><<<(unsigned)s.blocks, SORT_THREADS, 0, st>>>(s);
-        sort_scatter_kernel<true, ITEMS><<<(unsigned)s.blocks, SORT_THREADS, 0, st>>>(s);
-    } else {
-        sort_count_kernel<false, ITEMS><<<(unsigned)s.blocks, SORT_THREADS, 0, st>>>(s);
-        sort_scatter_kernel<false, ITEMS><<<(unsigned)s.blocks, SORT_THREADS, 0, st>>>(s);
-    }
+    sort_count_kernel<FIRST, ITEMS, DIGITS><<<(unsigned)s.blocks, SORT_THREADS, 0, st>>>(s);
+    allow_lds<&sort_scatter_kernel<FIRST, ITEMS, DIGITS>>(scatter_lds<DIGITS>());
+    sort_scatter_kernel<FIRST, ITEMS, DIGITS><<<(unsigned)s.blocks, SORT_THREADS, scatter_lds<DIGITS>(), st>>>(s);
+}
+void sort_pass(const SortPass& s, hipStream_t st) {
+    const bool few = s.items <= FEW_POSITIONS, first = s.shift == 0;
+    if (s.bits > MAX_DIGIT_BITS) sort_pass_t<true, FEW_ITEMS, WIDE_DIGITS>(s, st);
+    else if (few) first ? sort_pass_t<true, FEW_ITEMS, MAX_DIGITS>(s, st) : sort_pass_t<false, FEW_ITEMS, MAX_DIGITS>(s, st);
+    else first ? sort_pass_t<true, MANY_ITEMS, MAX_DIGITS>(s, st) : sort_pass_t<false, MANY_ITEMS, MAX_DIGITS>(s, st);
 }
 
 }  // namespace
@@ -650,7 +690,7 @@ EmbeddingPlan embedding_plan(int64_t positions, int64_t d, int64_t V, int dtype)
     EmbeddingPlan p;
     int bits = 1;
     while (((int64_t)1 << bits) < V) ++bits;
-    p.passes = (bits + MAX_DIGIT_BITS - 1) / MAX_DIGIT_BITS;
+    p.passes = bits <= WIDE_BITS && positions > ONE_BLOCK_SORT && positions <= WIDE_POSITIONS ? 1 : (bits + MAX_DIGIT_BITS - 1) / MAX_DIGIT_BITS;
     p.bits = (bits + p.passes - 1) / p.passes;
     p.tile = sort_tile(positions);
     p.blocks = (positions + p.tile - 1) / p.tile;
@@ -692,8 +732,7 @@ void launch_embedding_bwd(const EmbeddingArgs& a, const EmbeddingPlan& p, void* 
             s.shift = pass * p.bits;
             s.key_in = (const int32_t*)(w + p.key[to ^ 1]); s.pos_in = (const int32_t*)(w + p.pos[to ^ 1]);
             s.key_out = (int32_t*)(w + p.key[to]); s.pos_out = (int32_t*)(w + p.pos[to]);
-            if (a.positions <= FEW_POSITIONS) sort_pass_t<FEW_ITEMS>(s, st);
-            else sort_pass_t<MANY_ITEMS>(s, st);
+            sort_pass(s, st);
         }
     }
     SumArgs u{};

@@ -147,6 +147,10 @@ BWD = [  # dtype, N, T, d, V, ids, mask, dw
     ("f32", 1, 1, 1, 1, "one", "none", "f32"), ("f32", 5, 40, 3, 7, "zipf", "holes", "bf16"), ("f32", 3, 900, 256, 4096, "zipf", "ragged", "f32"),
     ("f32", 70, 500, 63, 1000, "uniform", "holes", "f32"), ("f32", 9, 1000, 132, 40, "one", "ragged", "bf16"), ("f32", 2, 30, 2050, 9, "zipf", "none", "f32"),
     ("f32", 6, 11, 20, 262145, "uniform", "none", "f32"),
+    # one pass over up to 12 bits of the id: sizes and vocabularies at its ends, runs over many stretches
+    ("bf16", 1, 8193, 8, 513, "uniform", "none", "f32"), ("f32", 32, 1024, 20, 4096, "zipf", "none", "f32"), ("bf16", 32, 1024, 16, 4097, "zipf", "holes", "f32"),
+    ("f32", 40, 500, 7, 1024, "one", "holes", "f32"), ("bf16", 30, 1000, 136, 3000, "zipf", "ragged", "bf16"), ("bf16", 1, 32769, 8, 2048, "zipf", "none", "f32"),
+    ("bf16", 9, 1000, 8, 4000, "zipf", "empty", "f32"), ("f32", 25, 1300, 5, 600, "one", "none", "bf16"),
 ]
 
 
