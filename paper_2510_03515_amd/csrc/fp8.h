@@ -73,6 +73,10 @@ __device__ __forceinline__ Raw8<float> load8(const float* row, int64_t c, int64_
     if (d % 4 == 0) {
         if (c < d) r.a = *(const float4*)(row + c);
         if (c + 4 < d) r.b = *(const float4*)(row + c + 4);
+    } else if (c + 8 <= d) {            // (16-byte loads take any address that is a multiple of 4)
+        typedef float any4 __attribute__((ext_vector_type(4), aligned(4)));
+        r.a = __builtin_bit_cast(float4, *(const any4*)(row + c));
+        r.b = __builtin_bit_cast(float4, *(const any4*)(row + c + 4));
     } else {
         float* p[8] = {&r.a.x, &r.a.y, &r.a.z, &r.a.w, &r.b.x, &r.b.y, &r.b.z, &r.b.w};
 #pragma unroll

@@ -26,8 +26,10 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const T* __restrict_
     if (bad && dev_status) atomicOr(dev_status, RAPID_STATUS_NONFINITE_VALUE);
 }
 
-// rows that do not begin on 16 bytes
+// rows that do not begin on 16 bytes (a type's vectors of any alignment are loaded as the chip allows it)
 __device__ __forceinline__ Raw8<bf16_t> load8_any(const bf16_t* row, int64_t c, int64_t n) {
+    typedef unsigned any4 __attribute__((ext_vector_type(4), aligned(2)));
+    if (c + 8 <= n) return Raw8<bf16_t>{__builtin_bit_cast(uint4, *(const any4*)(row + c))};
     uint32_t w[4];
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -35,6 +37,8 @@ __device__ __forceinline__ Raw8<bf16_t> load8_any(const bf16_t* row, int64_t c, 
     return Raw8<bf16_t>{make_uint4(w[0], w[1], w[2], w[3])};
 }
 __device__ __forceinline__ Raw8<float> load8_any(const float* row, int64_t c, int64_t n) {
+    typedef float any4 __attribute__((ext_vector_type(4), aligned(4)));
+    if (c + 8 <= n) return Raw8<float>{__builtin_bit_cast(float4, *(const any4*)(row + c)), __builtin_bit_cast(float4, *(const any4*)(row + c + 4))};
     float f[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) f[e] = c + e < n ? row[c + e] : 0.f;

@@ -142,16 +142,29 @@ __device__ __forceinline__ void pack_row_fp8(const RowsArgs& a, int64_t j, int64
     const uint8_t* ws = a.w_scales + (int64_t)token * scale_row;
     float acc = 0.f;
     bool bad = false;
+    // a trip of 512 columns is asked for before the one in front of it is worked on
+    Raw8<T> x_next;
+    uint2 w_next;
+    uint32_t scale_next;
+    auto ask = [&](int64_t c) {
+        x_next = load8(src, c, a.d);
+        w_next = make_uint2(0u, 0u);
+        scale_next = 127u;
+        if (c < bytes) {
+            w_next = *(const uint2*)(w + c);
+            scale_next = ws[c / FP8_BLOCK];
+        }
+    };
+    ask(lane * 8);
     for (int64_t base = 0; base < bytes; base += 512) {
         const int64_t c = base + lane * 8;
         float x[8], h[4], g[4];
-        load8(src, c, a.d, x);
-        uint2 wv = make_uint2(0u, 0u);
-        uint32_t w_scale = 127u, s;
-        if (c < bytes) {
-            wv = *(const uint2*)(w + c);
-            w_scale = ws[c / FP8_BLOCK];
-        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = x_next[e];
+        const uint2 wv = w_next;
+        const uint32_t w_scale = scale_next;
+        uint32_t s;
+        if (base + 512 < bytes) ask(c + 512);
         const uint2 q = quantize_block(x, s, bad);
         if (c < bytes) *(uint2*)(dst + c) = q;
         float part = 0.f;
