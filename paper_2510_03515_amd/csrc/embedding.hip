@@ -13,21 +13,25 @@ namespace rapid {
 
 namespace {
 
-// A row is worked on in pieces: 16 bytes, or (fp32 rows whose length is no multiple of 16 bytes) one element.
-struct BF16x8 { static constexpr int N = 8; typedef bf16_t elem; typedef uint4 raw;
+// A row is worked on in pieces: 16 bytes, or (fp32 rows whose length is no multiple of 16 bytes) one element, in the lookup 16 bytes at any multiple of
+// 4, the row's last piece moved back to end with it: the columns that it shares with the one before are written twice, with the same values.
+struct BF16x8 { static constexpr int N = 8; static constexpr bool ANY = false; typedef bf16_t elem; typedef uint4 raw;
     static __device__ __forceinline__ void get(const raw& v, float (&f)[8]) { unpack8(v, f); }
     static __device__ __forceinline__ raw put(const float (&f)[8]) { return pack8(f); } };
-struct F32x4 { static constexpr int N = 4; typedef float elem; typedef float4 raw;
+struct F32x4 { static constexpr int N = 4; static constexpr bool ANY = false; typedef float elem; typedef float4 raw;
     static __device__ __forceinline__ void get(const raw& v, float (&f)[4]) { f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w; }
     static __device__ __forceinline__ raw put(const float (&f)[4]) { return make_float4(f[0], f[1], f[2], f[3]); } };
-struct F32x1 { static constexpr int N = 1; typedef float elem; typedef float raw;
+struct F32x1 { static constexpr int N = 1; static constexpr bool ANY = false; typedef float elem; typedef float raw;
     static __device__ __forceinline__ void get(const raw& v, float (&f)[1]) { f[0] = v; }
     static __device__ __forceinline__ raw put(const float (&f)[1]) { return f[0]; } };
+struct F32x4Any { static constexpr int N = 4; static constexpr bool ANY = true; typedef float elem; typedef float raw __attribute__((ext_vector_type(4), aligned(4)));
+    static __device__ __forceinline__ void get(const raw& v, float (&f)[4]) { f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w; }
+    static __device__ __forceinline__ raw put(const float (&f)[4]) { return raw{f[0], f[1], f[2], f[3]}; } };
 
 // 16 bytes (or an element) that nobody reads before they have left the caches: stored past them, read without keeping them
 template <class R>
 __device__ __forceinline__ void store_past(R* to, const R& v) {
-    if constexpr (sizeof(R) == 16) {
+    if constexpr (alignof(R) == 16) {
         typedef unsigned u4 __attribute__((ext_vector_type(4)));
         __builtin_nontemporal_store(__builtin_bit_cast(u4, v), (u4*)to);
     } else {
@@ -62,8 +66,8 @@ __device__ __forceinline__ int valid_token(const int32_t* __restrict__ tokens, c
 template <class P, bool PAST, int U>
 __global__ __launch_bounds__(256) void embedding_fwd_kernel(const typename P::elem* __restrict__ table, const int32_t* __restrict__ tokens,
                                                             const uint8_t* __restrict__ mask, int64_t positions, int pieces, int V,
-                                                            float scale, typename P::elem* __restrict__ out,
-                                                            int32_t* __restrict__ dev_status, int rows, int step_rows, int step_pieces) {
+                                                            float scale, typename P::elem* __restrict__ out, int32_t* __restrict__ dev_status,
+                                                            int rows, int step_rows, int step_pieces, int d) {
     typedef typename P::raw raw;
     const int lane = threadIdx.x & 63;
     const int64_t p0 = ((int64_t)blockIdx.x * 4 + (threadIdx.x >> 6)) * rows;
@@ -71,16 +75,17 @@ __global__ __launch_bounds__(256) void embedding_fwd_kernel(const typename P::el
     const int n = (int)min((int64_t)rows, positions - p0);
     const int tok = lane < n ? valid_token(tokens, mask, p0 + lane, V, dev_status) : -1;
     int row = lane / pieces, piece = lane - row * pieces;
-    raw* dst = (raw*)out + p0 * pieces;
-    const raw* src = (const raw*)table;
+    typename P::elem* dst = out + p0 * d;
     for (int base = 0; base < n * pieces; base += 64 * U) {
         raw v[U];
-        int t[U];
+        int t[U], at[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
+            const int column = P::ANY ? min(piece * P::N, d - P::N) : piece * P::N;
+            at[u] = row * d + column;
             t[u] = __shfl(tok, row < n ? row : 0, 64);
             v[u] = raw{};
-            if (t[u] >= 0) v[u] = src[(int64_t)t[u] * pieces + piece];
+            if (t[u] >= 0) v[u] = *(const raw*)(table + (int64_t)t[u] * d + column);
             row += step_rows;
             piece += step_pieces;
             if (piece >= pieces) { piece -= pieces; ++row; }
@@ -93,8 +98,8 @@ __global__ __launch_bounds__(256) void embedding_fwd_kernel(const typename P::el
             P::get(v[u], f);
 #pragma unroll
             for (int e = 0; e < P::N; ++e) f[e] = t[u] < 0 ? 0.f : f[e] * scale;
-            if (PAST) store_past(dst + i, P::put(f));
-            else dst[i] = P::put(f);
+            if (PAST) store_past((raw*)(dst + at[u]), P::put(f));
+            else *(raw*)(dst + at[u]) = P::put(f);
         }
     }
 }
@@ -102,7 +107,7 @@ __global__ __launch_bounds__(256) void embedding_fwd_kernel(const typename P::el
 constexpr int64_t BEYOND_CACHES = (int64_t)256 << 20;      // bytes of the memory-side cache
 template <class P>
 void fwd_t(const EmbeddingArgs& a, const void* table, void* out, hipStream_t st) {
-    const int pieces = (int)(a.d / P::N);
+    const int pieces = (int)((a.d + P::N - 1) / P::N);
     // A wave takes a row, in trips of U pieces a lane with as few lanes left over as can be, or the rows that make up a trip of 4.  (256 x 2048 x 1536,
     // 3 pieces a lane, cold tables: U = 3 387 us, U = 4 411; 2, 4 and 8 rows a wave with U = 3: 385, 416, 454.)  A launch holds less than 2^32 threads.
     const int trips = (pieces + 63) / 64;
@@ -113,7 +118,7 @@ void fwd_t(const EmbeddingArgs& a, const void* table, void* out, hipStream_t st)
     const bool past = a.positions * a.d * (int64_t)sizeof(typename P::elem) > BEYOND_CACHES;
     auto go = [&](auto* kernel) {
         kernel<<<(unsigned)((waves + 3) / 4), 256, 0, st>>>((const typename P::elem*)table, a.tokens, a.mask, a.positions, pieces, (int)a.V, a.scale,
-                                                             (typename P::elem*)out, a.dev_status, rows, 64 / pieces, 64 % pieces);
+                                                             (typename P::elem*)out, a.dev_status, rows, 64 / pieces, 64 % pieces, (int)a.d);
     };
     if (trips == 2) past ? go(&embedding_fwd_kernel<P, true, 2>) : go(&embedding_fwd_kernel<P, false, 2>);
     else if (trips > 1 && (trips + 2) / 3 * 3 < (trips + 3) / 4 * 4) past ? go(&embedding_fwd_kernel<P, true, 3>) : go(&embedding_fwd_kernel<P, false, 3>);
@@ -683,6 +688,7 @@ void sort_pass(const SortPass& s, hipStream_t st) {
 void launch_embedding_fwd(const EmbeddingArgs& a, const void* table, void* out, hipStream_t st) {
     if (a.dtype == RAPID_DTYPE_BF16) fwd_t<BF16x8>(a, table, out, st);
     else if (a.d % 4 == 0) fwd_t<F32x4>(a, table, out, st);
+    else if (a.d > 4) fwd_t<F32x4Any>(a, table, out, st);
     else fwd_t<F32x1>(a, table, out, st);
 }
 
