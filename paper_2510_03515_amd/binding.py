@@ -172,18 +172,20 @@ def _need(t, dtype, name):
 
 
 def _shape(t, shape, name):
-    if tuple(t.shape) != tuple(shape):
-        raise TypeError(f"{name}: shape {tuple(t.shape)}, need {tuple(shape)}")
+    if t.shape != shape:
+        raise TypeError(f"{name}: shape {tuple(t.shape)}, need {shape}")
 
 
 def _here(tensors, dev_status, workspace=None):
     """The library works on the current device's current stream, sets bits of one int32 and takes workspaces by their bytes."""
     if dev_status is not None:
         _need(dev_status, torch.int32, "dev_status"); _shape(dev_status.view(-1)[:1], (1,), "dev_status")
+        tensors += (dev_status,)
     if workspace is not None:
         _need(workspace, torch.uint8, "workspace")
+        tensors += (workspace,)
     dev = torch.cuda.current_device()
-    for t in (*tensors, dev_status, workspace):
+    for t in tensors:
         if t is not None and t.get_device() != dev:
             raise TypeError(f"a tensor lies on {t.device}, the current device is {dev}")
 
@@ -323,8 +325,9 @@ def rapid_embedding_fwd(table, tokens, mask=None, scale=1.0, out=None, dev_statu
     if mask is not None:
         _need(mask, torch.uint8, "mask"); _shape(mask, (N, T), "mask")
     if out is None:
-        out = torch.empty((N, T, d), dtype=table.dtype, device=table.device)
-    _need(out, table.dtype, "out"); _shape(out, (N, T, d), "out")
+        out = table.new_empty((N, T, d))
+    else:
+        _need(out, table.dtype, "out"); _shape(out, (N, T, d), "out")
     _here((table, tokens, mask, out), dev_status)
     _check(load().rapid_embedding_fwd(_ptr(table), _ptr(tokens), _ptr(mask), N, T, d, V, _dtype_code(table), float(scale),
                                       _ptr(out), _ptr(dev_status), _stream()))
