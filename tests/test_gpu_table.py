@@ -528,3 +528,18 @@ def test_logprob_tile_order_changes_nothing(rb, key, values):
             assert torch.equal(p, want) and torch.equal(s, want_lse), value
     finally:
         rb.load().rapid_set_tuning(key, {10: 4, 13: 64}[key])
+
+
+@pytest.mark.parametrize("N,T,d", [(64, 1030, 1021), (64, 1030, 1024), (3, 7, 5), (3, 7, 6), (900, 70, 7), (2, 20000, 2), (16, 4000, 1049)])
+def test_fp32_rows_of_any_length_past_the_caches(rb, N, T, d):
+    """fp32 lookups of rows off 16-byte boundaries, outputs on both sides of 256 MB: the table's rows, and nothing beside them; their gradient sums to as much."""
+    V = 901
+    table = torch.randn(V, d, device="cuda")
+    tokens = torch.randint(0, V, (N, T), dtype=torch.int32, device="cuda")
+    mask = (torch.rand(N, T, device="cuda") < 0.9).to(torch.uint8)
+    out, untouched = _guarded((N, T, d), torch.float32)
+    rb.rapid_embedding_fwd(table, tokens, mask, out=out)
+    assert untouched() and torch.equal(out, table[tokens.long()] * (mask[:, :, None] != 0))
+    count = torch.bincount(tokens[mask != 0].long(), minlength=V).float()
+    grad = rb.rapid_embedding_bwd(torch.ones_like(out), tokens, mask, V)
+    assert torch.equal(grad, count[:, None].expand(V, d))        # small whole numbers: exact in fp32
