@@ -929,6 +929,7 @@ int64_t rapid_logits_cache_rows(int64_t N, int64_t T, int64_t d, int64_t V, int6
 // calls whose workspace has one size
 static size_t one_size_workspace(int op, int64_t N, int64_t T, int64_t d, int64_t V, int dtype) {
     if ((dtype != RAPID_DTYPE_F32 && dtype != RAPID_DTYPE_BF16) || !table_shape(N, T, d, V)) return 0;
+    if (dtype == RAPID_DTYPE_BF16 && d % 8 != 0) return 0;      // not a whole piece a row: the call is refused, and a plan of it divides by 0
     if (op == RAPID_OP_EMBEDDING_BWD) return embedding_plan(N * T, d, V, dtype).total;
     Fp8Plan p;
     return make_fp8_plan(p, N, T, d, V) ? p.total : 0;

@@ -163,3 +163,12 @@ def test_binding_refuses_other_devices_status_words_and_workspaces(rb, monkeypat
                  ((On(1),), None, On(0, torch.uint8)), ((On(1),), None, On(1, torch.float32)), ((On(1),), None, On(1, torch.uint8, contiguous=False))):
         with pytest.raises(TypeError):
             rb._here(*args)
+
+
+def test_sizes_of_calls_that_are_refused(rb):
+    """bf16 rows that are no multiple of 8 columns, shorter than one piece among them: no size, and no fault."""
+    for op in (rb.OP_EMBEDDING_BWD, rb.OP_LOGPROB_FWD_FP8):
+        for d in (1, 4, 7, 9, 12, 65535):
+            for minimum in (False, True):
+                assert rb.rapid_workspace_bytes(op, 2, 3, d, 9, 1, BF16, minimum=minimum) == 0
+                assert rb.rapid_workspace_bytes(op, 2, 3, d, 9, 1, F32, minimum=minimum) > 0
