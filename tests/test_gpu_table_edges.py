@@ -1,0 +1,123 @@
+"""The calls on a tied model's table with inputs that leave a kernel no room: sums that are exact in any order, so that one column, row or scale out of
+place shows.
+
+Coded heads.  W[v] is a random row of +-2^u (u 0 or 1 per block of 128), times 2^-s of the block; a hidden row is aligned with one row of W, m = 1, 2 or 3
+times its signs and 2^t (t 0, 1 or 2 per row and block), times 2^s of the block.  Values of a block keep their 4 bits in e4m3, products are whole numbers (times
+1, 2 or 4, the same in a group of eight), so nothing is cut off and every logit is a whole number below 2^24.  What is left
+of the bound is the log-sum-exp: roundings of the scaled exponent (a few 2^-24 of the largest |logit|), of its fp32 additions (128 at most in a slot) and
+of the exponentials (2^-16 in all), and of the results: 2^-16 + 2^-21 (1 + top + |ref|).
+The temperature is such that the aligned entry of the vocabulary has about half of the probability: counting it twice or not at all moves the
+log-sum-exp by some 0.4.
+"""
+import numpy as np
+import pytest
+import torch
+
+TYPES = {"bf16": torch.bfloat16, "f32": torch.float32}
+
+
+@pytest.fixture(scope="module")
+def rb():
+    from paper_2510_03515_amd import binding
+    binding.load()
+    assert torch.cuda.is_available()
+    return binding
+
+
+def _edges(V):
+    """Entries at the ends of 32-wide blocks, tiles of 128 and 256, and of the last tiles, which begin where they end with the vocabulary."""
+    at = [V - 1, V - 256, 256 * (V // 256) - 1, 256 * (V // 256), V - 128, 128 * (V // 128) - 1, 128 * (V // 128), 0, V - 2, V - 32, V - 33, V - 64, V - 65, V - 129,
+          V - 257, 31, 32, 127, 128, 255, 256, V // 2]
+    return [v for v in dict.fromkeys(at) if 0 <= v < V]
+
+
+def _coded(dtype, N, T, d, V, spread=20):
+    """hidden [N,T,d], W [V,d], targets, tokens [N,T], temperature; and the whole logits [N T, V] in float64."""
+    gen = torch.Generator().manual_seed(N * 7919 + T * 31 + d + V)
+    M, blocks = N * T, -(-d // 128)
+    per = lambda x: x.repeat_interleave(128, -1)[..., :d]
+    s = per(torch.randint(-spread, spread + 1, (blocks,), generator=gen).double())
+    sign = torch.randint(0, 2, (V, d), generator=gen).double() * 2 - 1
+    W = sign * torch.exp2(per(torch.randint(0, 2, (V, blocks), generator=gen).double()))
+    edges = _edges(V)
+    target = torch.randint(0, V, (M,), generator=gen)
+    target[:len(edges)] = torch.tensor(edges[:M])
+    size = torch.randint(1, 4, (M, d), generator=gen).double()
+    size[:, ::128] = 3.0                                            # (the largest of a block does not hang on the draw)
+    hidden = sign[target] * size * torch.exp2(per(torch.randint(0, 3, (M, blocks), generator=gen).double()))
+    z = (hidden @ W.t()).numpy()
+    temp = float(np.float32(z[np.arange(M), target.numpy()].mean() / (np.log(V) + 2.0)))
+    tokens = torch.where(torch.rand(M, generator=gen) < 0.7, target, torch.randint(0, V, (M,), generator=gen))
+    cast = lambda x, e: (x * torch.exp2(e)).to(torch.float32).to(TYPES[dtype])
+    return cast(hidden, s).view(N, T, d), cast(W, -s), tokens.to(torch.int32).view(N, T), temp, z
+
+
+def _log_probs(z, tokens, temp, weight=None):
+    """(logp, lse, bound) of logits; weight: how often an entry of the vocabulary is counted."""
+    z = z / temp
+    top = np.abs(z).max(axis=1)
+    zy, most = z[np.arange(len(z)), tokens.reshape(-1).numpy()], z.max(axis=1)
+    z -= most[:, None]
+    np.exp(z, out=z)
+    lse = np.log(z.sum(axis=1) if weight is None else z @ weight) + most
+    bound = lambda ref: 2.0 ** -16 + 2.0 ** -21 * (1 + top + np.abs(ref))
+    return zy - lse, lse, bound
+
+
+HEADS = {   # by the kernel that the sizes choose: dtype, N, T, d, V
+    "small head": [("bf16", 5, 13, 520, 70), ("bf16", 5, 13, 1032, 255), ("bf16", 2, 40, 1536, 255), ("bf16", 3, 50, 128, 257), ("bf16", 2, 30, 72, 513),
+                   ("bf16", 1, 300, 1024, 200), ("bf16", 3, 400, 512, 129), ("f32", 2, 20, 513, 129)],
+    "32 rows": [("bf16", 4, 8, 520, 256), ("bf16", 1, 32, 1032, 257), ("bf16", 8, 4, 264, 385), ("bf16", 1, 32, 1536, 511), ("bf16", 31, 1, 512, 255 + 128),
+                ("f32", 3, 7, 1001, 640), ("bf16", 2, 16, 136, 33000), ("bf16", 2, 16, 264, 70001)],
+    "64 rows": [("bf16", 8, 8, 520, 513), ("bf16", 1, 33, 1024, 383), ("bf16", 1, 64, 1536, 257), ("f32", 5, 9, 515, 1023), ("bf16", 4, 16, 136, 66049)],
+    "few row tiles": [("bf16", 1, 65, 520, 256), ("bf16", 5, 100, 1032, 257), ("bf16", 3, 300, 1536, 511), ("bf16", 2, 512, 264, 1025), ("bf16", 4, 64, 512, 300),
+                      ("f32", 4, 40, 1001, 769), ("bf16", 1, 290, 136, 50021)],
+    "row tiles": [("bf16", 2, 700, 520, 300), ("bf16", 1, 1100, 1536, 257), ("bf16", 3, 500, 1032, 511), ("bf16", 2, 1000, 1024, 768), ("bf16", 4, 300, 136, 2049),
+                  ("f32", 2, 600, 1001, 513), ("bf16", 1, 1025, 512, 256), ("bf16", 11, 100, 136, 70001)],
+}
+CASES = [c for cases in HEADS.values() for c in cases]
+
+
+@pytest.mark.parametrize("dtype,N,T,d,V", [c for c in CASES if c[1] * c[2] * c[4] <= 3000000])
+def test_oracle_sees_one_column(dtype, N, T, d, V):
+    """On the CPU: an entry left out, or the entries that the last two tiles share counted twice, is far outside of the bound of some row."""
+    _, _, tokens, temp, z = _coded(dtype, N, T, d, V)
+    assert np.abs(z).max() < 2 ** 24
+    _, lse, bound = _log_probs(z, tokens, temp)
+    wrong = [np.where(np.arange(V) == V - 1, 0.0, 1.0), np.where(np.arange(V) >= V - 32, 0.0, 1.0), np.where(np.arange(V) == 0, 0.0, 1.0)]
+    for tile in (128, 256):
+        if V > tile and V % tile:
+            shared = (np.arange(V) >= V - tile) & (np.arange(V) < tile * (V // tile))
+            if shared.any():
+                wrong += [np.where(shared, 2.0, 1.0), np.where(shared, 0.0, 1.0)]
+    for weight in wrong:
+        off = np.abs(_log_probs(z, tokens, temp, weight)[1] - lse)
+        assert (off > 100 * bound(lse)).any()
+
+
+def _scored(rb, hidden, W, tokens, temp, exact=True):
+    q = rb.rapid_quantize_fp8(W.cuda(), w_layout=rb.W_VD)
+    if exact:                                                        # nothing was rounded
+        blocks = q.values.shape[1] // 128
+        back = (q.values.double().view(W.shape[0], blocks, 128) * torch.exp2(q.scales[:, :blocks].double() - 127)[:, :, None]).view(W.shape[0], -1)
+        assert torch.equal(back[:, :W.shape[1]].cpu(), W.double()) and not back[:, W.shape[1]:].any()
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    mask = torch.ones(tokens.shape, dtype=torch.uint8, device="cuda")
+    logp, lse = rb.rapid_logprob_fwd_fp8(hidden.cuda(), q, tokens.cuda(), mask, temperature=temp, want_lse=True, dev_status=status)
+    return logp.double().cpu().numpy().reshape(-1), lse.double().cpu().numpy().reshape(-1), status.item()
+
+
+def _check_coded(rb, dtype, N, T, d, V, **kw):
+    hidden, W, tokens, temp, z = _coded(dtype, N, T, d, V, **kw)
+    print(f"coded head {dtype} {N}x{T} d={d} V={V} {kw}", flush=True)
+    logp, lse, status = _scored(rb, hidden, W, tokens, temp)
+    want_p, want_s, bound = _log_probs(z, tokens, temp)
+    assert status == 0
+    assert np.all(np.abs(lse - want_s) <= bound(want_s))
+    assert np.all(np.abs(logp - want_p) <= bound(want_p)) and np.all(logp <= 0.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,N,T,d,V", CASES)
+def test_every_column_counts_once(rb, dtype, N, T, d, V):
+    _check_coded(rb, dtype, N, T, d, V)
