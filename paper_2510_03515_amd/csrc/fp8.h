@@ -26,7 +26,6 @@ __device__ __forceinline__ uint32_t block_scale(uint32_t most) {
     return (uint32_t)(e < 1 ? 1 : e);
 }
 __device__ __forceinline__ float scale_inverse(uint32_t byte) { return __builtin_bit_cast(float, (254u - byte) << 23); }
-__device__ __forceinline__ float scale_value(uint32_t byte) { return __builtin_bit_cast(float, byte << 23); }
 
 // 4 values, scaled and rounded
 __device__ __forceinline__ uint32_t to_fp8x4(float a, float b, float c, float d, float inverse) {

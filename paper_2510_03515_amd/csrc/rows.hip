@@ -131,7 +131,7 @@ __device__ __forceinline__ void pack_row(const RowsArgs& a, int64_t j, int64_t p
 }
 
 // The same with 8-bit rows (fp8.h): H8[j] = hidden row `pos` in blocks of 128 with their scales, and zy[j] the product of what was stored with the
-// token's 8-bit weights, summed in fp32 (a block's sum takes its scale at once; then a fixed tree over the lanes).
+// token's 8-bit weights, summed in fp32 (a block's sum takes both its scales at once, since one of them alone may carry it out of range; then a fixed tree over the lanes).
 template <class T>
 __device__ __forceinline__ void pack_row_fp8(const RowsArgs& a, int64_t j, int64_t pos, int token) {
     const int lane = threadIdx.x & 63;
@@ -174,7 +174,7 @@ __device__ __forceinline__ void pack_row_fp8(const RowsArgs& a, int64_t j, int64
         from_fp8x4(q.y, h); from_fp8x4(wv.y, g);
 #pragma unroll
         for (int e = 0; e < 4; ++e) part = fmaf(h[e], g[e], part);
-        acc = fmaf(part * scale_value(s), scale_value(w_scale), acc);
+        acc += __builtin_amdgcn_ldexpf(part, (int)(s + w_scale) - 254);
         const uint32_t word = scale_word(s);
         if (lane == 0) *(uint32_t*)(a.h_scales + j * scale_row + base / FP8_BLOCK) = word;
     }

@@ -37,6 +37,8 @@ def _coded(dtype, N, T, d, V, spread=20):
     M, blocks = N * T, -(-d // 128)
     per = lambda x: x.repeat_interleave(128, -1)[..., :d]
     s = per(torch.randint(-spread, spread + 1, (blocks,), generator=gen).double())
+    if spread > 100:                                                # the largest scale of one side meets the smallest of the other
+        s = per(torch.where(torch.arange(blocks) % 2 == 0, float(spread), -float(spread) + 8).double())
     sign = torch.randint(0, 2, (V, d), generator=gen).double() * 2 - 1
     W = sign * torch.exp2(per(torch.randint(0, 2, (V, blocks), generator=gen).double()))
     edges = _edges(V)
@@ -121,3 +123,10 @@ def _check_coded(rb, dtype, N, T, d, V, **kw):
 @pytest.mark.parametrize("dtype,N,T,d,V", CASES)
 def test_every_column_counts_once(rb, dtype, N, T, d, V):
     _check_coded(rb, dtype, N, T, d, V)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,N,T,d,V", [("bf16", 2, 9, 264, 70), ("bf16", 4, 8, 520, 257), ("f32", 3, 20, 1001, 300), ("bf16", 3, 90, 264, 300), ("f32", 2, 600, 520, 511)])
+def test_scales_of_opposite_size(rb, dtype, N, T, d, V):
+    """Blocks of 2^118 against 2^-118: the block's product alone is out of fp32's range before the second scale, the logit is not."""
+    _check_coded(rb, dtype, N, T, d, V, spread=118)
