@@ -466,7 +466,8 @@ __device__ __forceinline__ void add_tile(f32x16 (&acc)[WJ], int seen, int hi4, f
         }
         mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
         const float nm = mx == -INFINITY ? 0.f : -mx * zs;
-        float sum = l[jb] * __builtin_amdgcn_exp2f(m[jb] == -INFINITY ? -INFINITY : fmaf(m[jb], zs, nm));
+        // (m - mx first: exactly 1 where the maximum stays, or the rounding of nm would be taken once more with every tile)
+        float sum = l[jb] * __builtin_amdgcn_exp2f(m[jb] == -INFINITY ? -INFINITY : (m[jb] - mx) * zs);
 #pragma unroll
         for (int v = 0; v < 16; ++v) sum += __builtin_amdgcn_exp2f(fmaf(acc[jb][v], zs, nm));
         m[jb] = mx;

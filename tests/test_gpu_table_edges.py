@@ -130,3 +130,22 @@ def test_every_column_counts_once(rb, dtype, N, T, d, V):
 def test_scales_of_opposite_size(rb, dtype, N, T, d, V):
     """Blocks of 2^118 against 2^-118: the block's product alone is out of fp32's range before the second scale, the logit is not."""
     _check_coded(rb, dtype, N, T, d, V, spread=118)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows", [16, 64])
+def test_log_sum_exp_does_not_drift_over_the_tiles(rb, rows):
+    """One entry of the first tile holds all the probability, and 15 or more further tiles of the same workgroup follow it.  Its logit Z and the temperature
+    1 are exact, so the log-sum-exp is Z but for the rounding of Z log2(e), once (2^-24 of Z), of the sum of one term and of the result (2^-24 of
+    Z again): 2^-23 Z + 2^-21."""
+    V, d = 128 * 256 * 16 + 1, 136
+    Z = [(a, w) for a in range(8, 16) for w in range(8, 16) if 512 <= 8 * a * w < 1024][:rows]
+    Z = (Z * rows)[:rows]
+    hidden, W = torch.zeros(1, rows, d), torch.zeros((V, d), dtype=torch.bfloat16)
+    for j, (a, w) in enumerate(Z):
+        hidden[0, j, 2 * j], W[j, 2 * j] = float(a), 8.0 * w
+    tokens = torch.arange(rows, dtype=torch.int32).view(1, rows)
+    logp, lse, status = _scored(rb, hidden.bfloat16(), W, tokens, 1.0, exact=False)
+    want = np.array([8.0 * a * w for a, w in Z])
+    assert status == 0 and np.all(np.abs(lse - want) <= 2.0 ** -23 * want + 2.0 ** -21)
+    assert np.all(np.abs(logp) <= 2.0 ** -23 * want + 2.0 ** -21) and np.all(logp <= 0.0)
