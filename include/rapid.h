@@ -395,7 +395,7 @@ int rapid_quantize_fp8(const void* W, int64_t d, int64_t V, int dtype, int w_lay
  * rapid_logprob_fwd under such a head.  The hidden rows (bf16 or fp32) are brought to 8 bits in the same way, in the call:
  *   z = sum over blocks b of 2^(e_hidden[b] + e_W[v,b]) * <e4m3 values of block b> / temperature
  *   logp_out[n,t] = z[y] - logsumexp(z) (at most 0), lse_out[n,t] = logsumexp(z) (may be NULL); 0 where mask = 0
- * z[y] is summed in fp32.  The logits of the log-sum-exp come from the 8-bit matrix unit, which adds eight neighbouring products
+ * z[y] is summed in fp32.  A row with a logit from 2.36e38 on (2^128 / log2(e)) has no finite results.  The logits of the log-sum-exp come from the 8-bit matrix unit, which adds eight neighbouring products
  * with the bits from 2^-13 of the largest on and everything else in fp32: about 1e-4 of the logits' spread, some
  * hundredths of what the rounding to e4m3 moves them by.
  * A token id outside [0,V) is treated as token 0 (RAPID_STATUS_BAD_TOKEN).  At most 2^25 positions.  Workspace:

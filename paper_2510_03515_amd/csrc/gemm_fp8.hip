@@ -56,8 +56,14 @@ __device__ __forceinline__ i32x8 whole(const Frag<NB>& f, int n) {
     return __builtin_bit_cast(i32x8, __builtin_shufflevector(f.lo[n], f.hi[n], 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
-// Per token row (one lane pair) the largest logit and the sum of exponentials over this wave's columns.  A logit that is NaN or +infinity (of values
-// that were not finite) makes the slot +infinity, so that the row's log-sum-exp is not finite either.
+// A logit that is NaN or +infinity (of values that were not finite) makes the sum NaN, one whose exponent is beyond fp32 (2^128 / log2(e) = 2.36e38 and more)
+// takes even its own term out of the sum.  Such a slot becomes +infinity, so that the row's log-sum-exp is not finite either.
+__device__ __forceinline__ void flag_slot(float& mx, float& sum) {
+    if (sum > 0.f || (sum == 0.f && mx == -INFINITY)) return;      // as it should be; no column at all
+    mx = INFINITY;
+    sum = 1.f;
+}
+// Per token row (one lane pair) the largest logit and the sum of exponentials over this wave's columns.
 template <class S, bool ALL>
 __device__ __forceinline__ void epilogue_rows(const Fp8FwdArgs& a, const Lane<S>& L, int64_t slot, int64_t j_tile, int n_valid, int n_seen,
                                               f32x16 (&acc)[S::WI][S::WJ]) {
@@ -83,7 +89,7 @@ __device__ __forceinline__ void epilogue_rows(const Fp8FwdArgs& a, const Lane<S>
 #pragma unroll
             for (int v = 0; v < 16; ++v) l += __builtin_amdgcn_exp2f(fmaf(value(ib, v), zs, nm));
         l += __shfl_xor(l, 32, 64);
-        if (l != l) { mx = INFINITY; l = 1.f; }
+        flag_slot(mx, l);
         if (L.hi == 0) {
             const int64_t j = j_tile + L.wave_j * (WJ * 32) + jb * 32 + L.lj;
             a.part_max[slot * a.ld_part + j] = mx * a.inv_temp;
@@ -475,7 +481,7 @@ __device__ __forceinline__ void add_tile(f32x16 (&acc)[WJ], int seen, int hi4, f
     }
 }
 // The workgroup's slot: the sums of a lane pair, then of the four waves that share rows from row0 on (wave: 0 .. 3 among them), in order.  `shared` has
-// 256 WJ floats for them; a NaN becomes +infinity (see epilogue_rows).
+// 256 WJ floats for them.
 template <int WJ>
 __device__ __forceinline__ void leave_slot(const Fp8FwdArgs& a, float* shared, int wave, int row0, float zs, float (&m)[WJ], float (&l)[WJ]) {
     const int lane = threadIdx.x & 63;
@@ -500,7 +506,7 @@ __device__ __forceinline__ void leave_slot(const Fp8FwdArgs& a, float* shared, i
             const float mw = shared[(w * WJ + jb) * 64 + lane], lw = shared[(w * WJ + jb) * 64 + 32 + lane];
             sum += lw == 0.f ? 0.f : lw * __builtin_amdgcn_exp2f((mw - mx) * zs);
         }
-        if (sum != sum) { mx = INFINITY; sum = 1.f; }
+        flag_slot(mx, sum);
         a.part_max[(int64_t)blockIdx.x * a.ld_part + row0 + jb * 32 + lane] = mx * a.inv_temp;
         a.part_sum[(int64_t)blockIdx.x * a.ld_part + row0 + jb * 32 + lane] = sum;
     }

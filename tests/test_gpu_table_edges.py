@@ -149,3 +149,22 @@ def test_log_sum_exp_does_not_drift_over_the_tiles(rb, rows):
     want = np.array([8.0 * a * w for a, w in Z])
     assert status == 0 and np.all(np.abs(lse - want) <= 2.0 ** -23 * want + 2.0 ** -21)
     assert np.all(np.abs(logp) <= 2.0 ** -23 * want + 2.0 ** -21) and np.all(logp <= 0.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("N,T,d,V", [(1, 3, 16, 90), (2, 8, 264, 700), (1, 40, 136, 300), (2, 100, 264, 300), (2, 600, 136, 513)])
+def test_logits_next_to_the_end_of_fp32(rb, N, T, d, V):
+    """A logit of 2.6e38 times log2(e) is beyond fp32: results are the formula's (whose log-probs are 0 and -2.6e38) or not finite, never a finite other value."""
+    hidden, W = torch.zeros(N, T, d), torch.zeros(V, d)
+    hidden[0, 0, 5], W[V - 1, 5] = 1.75 * 2.0 ** 63, 1.75 * 2.0 ** 63
+    hidden[0, 1, 5], W[0, 6] = 1.75 * 2.0 ** 63, 1.0
+    hidden[0, 2, 6] = 3.0
+    tokens = torch.zeros((N, T), dtype=torch.int32)
+    tokens[0, 0] = V - 1
+    logp, lse, _ = _scored(rb, hidden, W, tokens, 1.0, exact=False)
+    z = 3.0625 * 2.0 ** 126
+    for got, want in ((lse[0], z), (lse[1], z), (logp[0], 0.0), (logp[1], -z)):
+        assert not np.isfinite(got) or abs(got - want) <= 2.0 ** -22 * abs(want), (got, want)
+    rest = np.log(V - 1 + np.exp(3.0))
+    assert abs(lse[2] - rest) < 1e-4 and abs(logp[2] - (3.0 - rest)) < 1e-4      # the other rows are as they would be alone
+    assert np.all(np.abs(lse[3:] - np.log(V)) < 1e-4)
