@@ -168,3 +168,31 @@ def test_logits_next_to_the_end_of_fp32(rb, N, T, d, V):
     rest = np.log(V - 1 + np.exp(3.0))
     assert abs(lse[2] - rest) < 1e-4 and abs(logp[2] - (3.0 - rest)) < 1e-4      # the other rows are as they would be alone
     assert np.all(np.abs(lse[3:] - np.log(V)) < 1e-4)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("N,T,d,V", [(1, 20, 128, 200), (4, 8, 520, 3000), (1, 50, 1536, 700), (2, 200, 1024, 3000), (2, 700, 264, 2000)])
+def test_confident_tokens(rb, N, T, d, V):
+    """Sampled tokens with nearly all of the probability, logits 12 to 25: in every group of eight the aligned entry has one product of 448^2 and seven of 2^2, which the
+    matrix unit leaves out (each is below 2^-13 of the largest).  The log-sum-exp may be lower than the formula's by 28 / 448^2 of its
+    logit, never higher; the sampled logit is summed with all of it, and the log-prob is 0 where that comes out above."""
+    gen = torch.Generator().manual_seed(d + V)
+    M = N * T
+    groups = torch.where(torch.arange(d) % 8 == 0, 448.0, 2.0)
+    hidden = (groups * torch.where(torch.rand(M, 1, generator=gen) < 0.5, 1.0, 0.5)).view(N, T, d)       # powers of two: the same bits in e4m3
+    W = torch.zeros(V, d)
+    target = int(torch.randint(0, V, (1,), generator=gen))
+    W[target] = groups
+    tokens = torch.full((N, T), target, dtype=torch.int32)
+    top = float((groups * groups).sum())
+    temp = float(np.float32(top / 25.0))
+    logp, lse, status = _scored(rb, hidden.bfloat16(), W.bfloat16(), tokens, temp)
+    z = hidden[:, :, 0].double().numpy().reshape(-1) / 448.0 * top / temp
+    want = z + np.log1p((V - 1) * np.exp(-z))
+    cut = z * 28 / 448.0 ** 2
+    fp32 = 2.0 ** -16 + 2.0 ** -21 * (1 + 2 * z) + d * 2.0 ** -22 * z / 8
+    assert status == 0
+    assert np.all(lse <= want + fp32) and np.all(lse >= want - cut - fp32)
+    assert np.all(np.abs(logp - (z - want)) <= cut + fp32) and np.all(logp <= 0.0)
+    above = lse < z - fp32
+    assert above.any() and np.all(logp[above] == 0.0)
