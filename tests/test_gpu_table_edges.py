@@ -196,3 +196,48 @@ def test_confident_tokens(rb, N, T, d, V):
     assert np.all(np.abs(logp - (z - want)) <= cut + fp32) and np.all(logp <= 0.0)
     above = lse < z - fp32
     assert above.any() and np.all(logp[above] == 0.0)
+
+
+# ------------------------------------------------------------------------------ lookup and gradient of very many positions
+def _whole_rows(N, T, d, dtype):
+    """Gradient rows of small whole numbers that depend on position and column: every sum is exact in fp32."""
+    p, c = torch.arange(N * T, device="cuda")[:, None], torch.arange(d, device="cuda")[None, :]
+    return ((p * 31 + p // 64 * 5 + c * 17) % 7 - 3).to(TYPES[dtype]).view(N, T, d)
+
+
+def _zipf(N, T, V, seed):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    r = torch.exp(torch.rand((N, T), generator=gen, device="cuda", dtype=torch.float64) * np.log(V + 1)).long() - 1
+    return r.clamp(0, V - 1).to(torch.int32), (torch.rand((N, T), generator=gen, device="cuda") < 0.8).to(torch.uint8)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,N,T,d,V", [
+    ("bf16", 1300, 1000, 8, 5000), ("bf16", 1100, 2000, 8, 300000), ("f32", 1100, 1000, 5, 600),        # sorts with two and three rounds a block, one to three passes
+    ("f32", 64, 1030, 1021, 901), ("f32", 64, 1030, 1024, 901), ("bf16", 64, 2100, 1024, 5000)])         # gradient rows of more than 256 MB
+def test_gradient_of_many_positions(rb, dtype, N, T, d, V):
+    print(f"many positions {dtype} {N}x{T} d={d} V={V}", flush=True)
+    tokens, mask = _zipf(N, T, V, d)
+    dh = _whole_rows(N, T, d, dtype)
+    at = mask.view(-1).nonzero()[:, 0]
+    want = torch.zeros((V, d), dtype=torch.float64, device="cuda")
+    for part in at.split(1 << 18):
+        want.index_add_(0, tokens.view(-1)[part].long(), dh.view(-1, d)[part].double())
+    assert want.abs().max().item() < 2 ** 24
+    assert torch.equal(rb.rapid_embedding_bwd(dh, tokens, mask, V).double(), want)
+    old = (torch.arange(V * d, device="cuda") % 11).float().view(V, d)
+    got = rb.rapid_embedding_bwd(dh, tokens, mask, V, dtable=old.clone(), accumulate=True)
+    assert torch.equal(got.double(), want + old)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,N,T,d", [("bf16", 1, (1 << 25) + 5, 8), ("f32", 5, ((1 << 25) + 35) // 5, 3), ("f32", 1, (1 << 25) + 1, 5)])
+def test_lookup_of_many_positions(rb, dtype, N, T, d):
+    """More than 2^25 positions, where a wave takes 64 of them."""
+    V = 1013
+    table = torch.randn((V, d), device="cuda").to(TYPES[dtype])
+    tokens, mask = _zipf(N, T, V, d)
+    out = rb.rapid_embedding_fwd(table, tokens, mask)
+    for i in range(0, N * T, 1 << 22):
+        at = slice(i, i + (1 << 22))
+        assert torch.equal(out.view(-1, d)[at], table[tokens.view(-1)[at].long()] * (mask.view(-1)[at, None] != 0))
