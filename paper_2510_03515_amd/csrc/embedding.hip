@@ -112,7 +112,9 @@ void fwd_t(const EmbeddingArgs& a, const void* table, void* out, hipStream_t st)
     // 3 pieces a lane, cold tables: U = 3 387 us, U = 4 411; 2, 4 and 8 rows a wave with U = 3: 385, 416, 454.)  A launch holds less than 2^32 threads.
     const int trips = (pieces + 63) / 64;
     int rows = 256 / pieces < 1 ? 1 : trips > 1 ? 1 : 256 / pieces > 64 ? 64 : 256 / pieces;
-    if (a.positions <= 16384) rows = 1;                     // few: all under way together
+    // Few positions: all under way together.  Table in the caches, a row a wave and several: bf16, d = 64: 2048 positions 3.0 and 3.1 us, 4096 3.5 and
+    // 3.1; d = 512: 2048 3.2 and 3.3, 4096 3.9 and 3.6; fp32, d = 256: 2048 3.1 and 3.1, 4096 3.7 and 3.4.
+    if (a.positions <= 2048) rows = 1;
     if (a.positions > ((int64_t)1 << 25)) rows = 64;
     const int64_t waves = (a.positions + rows - 1) / rows;
     const bool past = a.positions * a.d * (int64_t)sizeof(typename P::elem) > BEYOND_CACHES;
