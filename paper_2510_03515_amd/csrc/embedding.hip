@@ -660,8 +660,16 @@ int pieces_of(int64_t d, int dtype) { return (int)(d / (dtype == RAPID_DTYPE_BF1
 
 // Items a thread takes in a round of the sort.  Few positions: more blocks with less to do each.
 constexpr int FEW_ITEMS = 2, MANY_ITEMS = 8;
-constexpr int64_t FEW_POSITIONS = 131072, ONE_BLOCK_SORT = 8192, WIDE_POSITIONS = 32768;
-static_assert(WIDE_POSITIONS <= 256 * SORT_THREADS * FEW_ITEMS, "a block of a wide pass has one round");
+// d = 64, whole gradients: with 2 items and with 8 65536 positions 62 and 72 us, 131072 97 and 105, 262144 142 and 142, 524288 147 and 142 (V = 151936).
+constexpr int64_t FEW_POSITIONS = 131072;
+// One pass over 10 to 12 bits and two of half as many, V = 4096: 8200 positions 23.8 and 30.1 us, 32768 38.2 and 39.1, 65536 62.9 and 59.7.
+constexpr int64_t WIDE_POSITIONS = 32768;
+static_assert(WIDE_POSITIONS <= 256 * SORT_THREADS * FEW_ITEMS && WIDE_POSITIONS <= FEW_POSITIONS, "a block of a wide pass has one round");
+// All passes in one block, and the launches of many.  Ids that many blocks sort in one pass: V = 4096: 2048 positions 18.8 and 19.1 us, 3072 20.1 and 19.6,
+// 8192 29.5 and 22.7; V = 300: 2048 16.4 and 17.4, 4097 21.4 and 19.9.  In two or more: V = 5000: 5120 26.2 and 26.4, 8192 31.8 and 31.2; V = 151936: 4096
+// 30.1 and 32.3, 6144 34.3 and 34.1, 8192 37.3 and 35.2.
+constexpr int64_t ONE_BLOCK_ONE_PASS = 2560, ONE_BLOCK_SORT = 6144;
+static_assert(ONE_BLOCK_ONE_PASS <= ONE_BLOCK_SORT && ONE_BLOCK_SORT <= 8 * ONE_THREADS, "a block holds its items in registers, 8 a thread");
 int64_t sort_tile(int64_t positions) {
     const int64_t round = SORT_THREADS * (positions <= FEW_POSITIONS ? FEW_ITEMS : MANY_ITEMS);
     const int64_t per = (positions + 255) / 256;            // at most 256 blocks: every block adds up the counts of all
@@ -698,7 +706,8 @@ EmbeddingPlan embedding_plan(int64_t positions, int64_t d, int64_t V, int dtype)
     EmbeddingPlan p;
     int bits = 1;
     while (((int64_t)1 << bits) < V) ++bits;
-    p.passes = bits <= WIDE_BITS && positions > ONE_BLOCK_SORT && positions <= WIDE_POSITIONS ? 1 : (bits + MAX_DIGIT_BITS - 1) / MAX_DIGIT_BITS;
+    p.one_block = positions <= (bits <= WIDE_BITS ? ONE_BLOCK_ONE_PASS : ONE_BLOCK_SORT);
+    p.passes = bits <= WIDE_BITS && !p.one_block && positions <= WIDE_POSITIONS ? 1 : (bits + MAX_DIGIT_BITS - 1) / MAX_DIGIT_BITS;
     p.bits = (bits + p.passes - 1) / p.passes;
     p.tile = sort_tile(positions);
     p.blocks = (positions + p.tile - 1) / p.tile;
@@ -729,7 +738,7 @@ void launch_embedding_bwd(const EmbeddingArgs& a, const EmbeddingPlan& p, void* 
     s.hist = (int32_t*)(w + p.hist); s.counts = (int32_t*)(w + p.counts);
     s.flags = accumulate ? nullptr : (uint32_t*)(w + p.flags); s.flag_words = (a.V + 3) / 4;
     s.items = a.positions; s.tile = p.tile; s.bits = p.bits; s.blocks = (int)p.blocks;
-    if (a.positions <= ONE_BLOCK_SORT) {
+    if (p.one_block) {
         s.key_out = (int32_t*)(w + p.key[0]); s.pos_out = (int32_t*)(w + p.pos[0]);
         if (a.positions <= ONE_THREADS) sort_one_t<1>(s, p.passes, st);
         else if (a.positions <= 4 * ONE_THREADS) sort_one_t<4>(s, p.passes, st);

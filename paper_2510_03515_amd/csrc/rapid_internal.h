@@ -407,6 +407,7 @@ void launch_embedding_fwd(const EmbeddingArgs& a, const void* table, void* out, 
 // how the backward sorts and shares out a batch of so many positions, and where its scratch lies
 struct EmbeddingPlan {
     int passes, bits;                  // radix passes and bits of the id in each
+    bool one_block;                    // all of them in one launch of one block
     int64_t tile, blocks;              // positions per block of a pass
     int64_t stretches, least_rows;     // groups of threads that share the sorted positions, and what a group gets at least
     size_t counts, key[2], pos[2], hist, flags, part, total;

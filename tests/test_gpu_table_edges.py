@@ -241,3 +241,31 @@ def test_lookup_of_many_positions(rb, dtype, N, T, d):
     for i in range(0, N * T, 1 << 22):
         at = slice(i, i + (1 << 22))
         assert torch.equal(out.view(-1, d)[at], table[tokens.view(-1)[at].long()] * (mask.view(-1)[at, None] != 0))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,positions,d,V", [
+    ("bf16", 2560, 16, 4096), ("bf16", 2561, 16, 4096), ("f32", 2561, 6, 513), ("bf16", 2561, 24, 512), ("f32", 3000, 8, 2), ("bf16", 2561, 8, 4097),
+    ("bf16", 6144, 16, 4097), ("bf16", 6145, 16, 4097), ("f32", 6145, 5, 300000), ("bf16", 6145, 8, 300), ("bf16", 32768, 8, 4096), ("bf16", 32769, 8, 4096)])
+@pytest.mark.parametrize("kept", [1.0, 0.5, 0.0])
+def test_gradient_on_both_sides_of_the_sorts(rb, dtype, positions, d, V, kept):
+    """The one-block sort, one wide pass and passes of many blocks, next to where one takes over from the other; few or no valid positions among them."""
+    print(f"sorts {dtype} {positions} d={d} V={V} {kept}", flush=True)
+    tokens, mask = _zipf(1, positions, V, positions + d)
+    mask *= (torch.rand((1, positions), generator=torch.Generator().manual_seed(d)) < kept).cuda()
+    if kept == 1.0:
+        tokens[0, 5], tokens[0, positions - 1] = V, -1               # ids without a row
+    dh = _whole_rows(1, positions, d, dtype)
+    good = (mask != 0) & (tokens >= 0) & (tokens < V)
+    want = torch.zeros((V, d), dtype=torch.float64, device="cuda").index_add_(0, tokens[good].long(), dh[good].double())
+    assert torch.equal(rb.rapid_embedding_bwd(dh, tokens, mask, V).double(), want)
+    assert torch.equal(rb.rapid_embedding_bwd(dh, tokens, mask, V, dtable=torch.ones((V, d), device="cuda"), accumulate=True).double(), want + 1.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,d", [("bf16", 8), ("bf16", 200), ("bf16", 1032), ("f32", 3), ("f32", 100), ("f32", 257)])
+def test_lookup_on_both_sides_of_several_rows_a_wave(rb, dtype, d):
+    table = torch.randn((333, d), device="cuda").to(TYPES[dtype])
+    for positions in (2047, 2048, 2049, 2112):
+        tokens, mask = _zipf(1, positions, 333, positions)
+        assert torch.equal(rb.rapid_embedding_fwd(table, tokens, mask), table[tokens.long()] * (mask[:, :, None] != 0))
