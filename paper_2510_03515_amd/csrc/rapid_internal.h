@@ -383,7 +383,7 @@ struct Fp8FwdArgs {       // 8-bit logits tile -> per-slot (max, sumexp), as Fwd
     int64_t row0;
     float inv_temp;
     const int32_t* counts;
-    float *part_max, *part_sum;       // [2 tilesV][ld_part]
+    float *part_max, *part_sum;       // [slots of Fp8Way][ld_part]
     int64_t ld_part;
     int gi;                           // tiles of the vocabulary that share one row tile before the order moves on
 };
