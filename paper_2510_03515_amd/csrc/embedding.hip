@@ -5,7 +5,6 @@
 //
 // Both are bound by memory.  The backward sorts the valid positions by (token, position) first, so that every row of dE is formed by one
 // owner, in one order that hangs on the valid positions alone: no floating-point atomics, the same bits in every run.
-#include "mfma_tiles.h"
 #include "rapid_internal.h"
 #include "row_math.h"
 

@@ -774,6 +774,21 @@ __device__ __forceinline__ void store_tile_through_lds(char* lds, const Lane<S>&
     }
 }
 
+// ragged last vocabulary tile: the columns that do not exist become -infinity
+template <class S>
+__device__ __forceinline__ void mask_padding(f32x16 (&acc)[S::WI][S::WJ], int n_valid, int hi) {
+    if (n_valid >= S::WI * 32) return;
+#pragma unroll
+    for (int ib = 0; ib < S::WI; ++ib)
+#pragma unroll
+        for (int jb = 0; jb < S::WJ; ++jb)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const int rel = ib * 32 + (v >> 2) * 8 + hi * 4 + (v & 3);
+                acc[ib][jb][v] = rel < n_valid ? acc[ib][jb][v] : -INFINITY;
+            }
+}
+
 // ------------------------------------------------------------------------------------- fwd_lse
 // STORE: also keep, for a backward that reloads them instead of recomputing the logits, the tile's
 // scaled probabilities u[j][v] = exp(z[j][v] - r[j]) in bf16 in a.zc.  The reference r[j] (a.refz) is

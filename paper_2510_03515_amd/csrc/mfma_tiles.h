@@ -3,8 +3,6 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include <atomic>
-
 namespace rapid {
 
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -86,33 +84,5 @@ struct Lane {
         lj = lane & 31;
     }
 };
-
-// Lets `kernel` use `bytes` of dynamic LDS: once per kernel and device (the attribute belongs to the
-// device's copy of the function), not once per launch.  One static bit mask per kernel.
-template <auto kernel>
-void allow_lds(int bytes) {
-    static std::atomic<uint64_t> done{0};
-    int dev = 0;
-    (void)hipGetDevice(&dev);
-    const uint64_t bit = 1ull << (dev & 63);
-    if (done.load(std::memory_order_acquire) & bit) return;
-    if (hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess)
-        done.fetch_or(bit, std::memory_order_release);
-}
-
-// ragged last vocabulary tile: the columns that do not exist become -infinity
-template <class S>
-__device__ __forceinline__ void mask_padding(f32x16 (&acc)[S::WI][S::WJ], int n_valid, int hi) {
-    if (n_valid >= S::WI * 32) return;
-#pragma unroll
-    for (int ib = 0; ib < S::WI; ++ib)
-#pragma unroll
-        for (int jb = 0; jb < S::WJ; ++jb)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const int rel = ib * 32 + (v >> 2) * 8 + hi * 4 + (v & 3);
-                acc[ib][jb][v] = rel < n_valid ? acc[ib][jb][v] : -INFINITY;
-            }
-}
 
 }  // namespace rapid

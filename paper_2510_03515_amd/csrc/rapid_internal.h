@@ -4,6 +4,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "rapid.h"
 
 namespace rapid {
@@ -17,6 +19,19 @@ static inline int64_t round_up(int64_t x, int64_t m) { return (x + m - 1) / m * 
 // operand tile are read for the same k at the same time; with an odd line stride they fall on
 // different L2 / HBM channels instead of piling onto one or two.
 static inline int64_t padded_ld(int64_t x) { return ((x / 64) % 2 == 0) ? x + 64 : x; }
+
+// Lets `kernel` use `bytes` of dynamic LDS: once per kernel and device (the attribute belongs to the
+// device's copy of the function), not once per launch.  One static bit mask per kernel.
+template <auto kernel>
+void allow_lds(int bytes) {
+    static std::atomic<uint64_t> done{0};
+    int dev = 0;
+    (void)hipGetDevice(&dev);
+    const uint64_t bit = 1ull << (dev & 63);
+    if (done.load(std::memory_order_acquire) & bit) return;
+    if (hipFuncSetAttribute((const void*)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess)
+        done.fetch_or(bit, std::memory_order_release);
+}
 
 // device counters written by the compaction step: [0] = M (valid tokens), [1] = M rounded up to 256
 enum { CNT_M = 0, CNT_MR = 1, CNT_WORDS = 64 };
