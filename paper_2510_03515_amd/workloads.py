@@ -74,6 +74,12 @@ def _torch_dtype(name):
     return {"f32": torch.float32, "bf16": torch.bfloat16}[name]
 
 
+def _draw(logits, gen):
+    """One id per row from softmax(logits), by the Gumbel-max trick."""
+    u = torch.rand(logits.shape, generator=gen, device=logits.device, dtype=torch.float32)
+    return (logits - torch.log((-torch.log(u.clamp_min(1e-30))).clamp_min(1e-30))).argmax(dim=1)
+
+
 def make_workload(spec: WorkloadSpec, seed: int = 0, device: str = "cpu", row_chunk: int = 4096):
     """Returns a dict of tensors on `device`:
     hidden [N,T,d] dtype, W [d,V] dtype, W_old [d,V] dtype, tokens [N,T] int32, mask [N,T] uint8,
@@ -156,8 +162,7 @@ def make_tied_workload(spec: WorkloadSpec, seed: int = 0, device: str = "cpu", s
     inputs, tokens = (torch.zeros((N, T), dtype=torch.int32, device=dev) for _ in range(2))
     for t in range(T):
         z = as_served((table[x].float() * scale).to(table.dtype)) @ head.t()
-        u = torch.rand(z.shape, generator=gen, device=dev)
-        y = (z - torch.log(-torch.log(u.clamp_min(1e-30)).clamp_min(1e-30))).argmax(dim=1)
+        y = _draw(z, gen)
         inputs[:, t], tokens[:, t] = x.to(torch.int32), y.to(torch.int32)
         x = y
     rewards = (torch.rand((N,), generator=gen, device=dev) < spec.reward_p).float()

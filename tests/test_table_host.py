@@ -172,3 +172,19 @@ def test_sizes_of_calls_that_are_refused(rb):
             for minimum in (False, True):
                 assert rb.rapid_workspace_bytes(op, 2, 3, d, 9, 1, BF16, minimum=minimum) == 0
                 assert rb.rapid_workspace_bytes(op, 2, 3, d, 9, 1, F32, minimum=minimum) > 0
+
+
+def test_tied_workload_draws_from_its_policy():
+    """Tokens of the tied workload by the previous token against softmax(scale E[x] . E): chi-squared over the ids, and the inputs are the tokens before."""
+    from paper_2510_03515_amd import workloads as wl
+    spec = wl.small_spec("tied", "f32", d=16, V=12, prompts=40, G=16, len_lo=30, len_hi=30)
+    w = wl.make_tied_workload(spec, seed=1, scale=4.0)
+    x, y, E = w["inputs"].long(), w["tokens"].long(), w["table"].double()
+    assert torch.equal(x[:, 1:], y[:, :-1]) and len(x[:, 0].unique()) > 5
+    p = torch.softmax(4.0 * E @ E.t(), dim=1)
+    seen = torch.zeros(12, 12, dtype=torch.float64)
+    seen.index_put_((x.reshape(-1), y.reshape(-1)), torch.ones(x.numel(), dtype=torch.float64), accumulate=True)
+    want = seen.sum(1, keepdim=True) * p
+    assert want.min() > 5                                             # enough in every cell for the statistic to be near its distribution
+    # 132 degrees of freedom: mean 132, standard deviation 16.2; 6 of them
+    assert ((seen - want) ** 2 / want).sum() < 132 + 6 * 16.2
