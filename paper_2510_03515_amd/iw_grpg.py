@@ -93,7 +93,7 @@ def served_in_8_bits(rows):
     return (q.values.float().view(rows.shape[0], blocks, 128) * scale[:, :, None]).view(rows.shape[0], -1)[:, :rows.shape[1]]
 
 
-def iw_grpg_tied(w, inner_steps=8, lr=2e-5, eta=2.0, coef_mode=1, logits_cache=False, optimizer="sgd"):
+def iw_grpg_tied(w, inner_steps=8, lr=0.02, eta=2.0, coef_mode=1, logits_cache=False, optimizer="sgd"):
     """iw_grpg on a tied table: `w` is the dict of workloads.make_tied_workload (device tensors, tokens drawn from the table
     served in 8 bits).  The table's gradient is the head's (dW, [V,d]) plus the lookup's, which is added to it in place."""
     spec, scale = w["spec"], w["scale"]
@@ -136,7 +136,7 @@ def iw_grpg_tied(w, inner_steps=8, lr=2e-5, eta=2.0, coef_mode=1, logits_cache=F
 def main():
     ap = argparse.ArgumentParser()
     ap.add_argument("--inner-steps", type=int, default=8)
-    ap.add_argument("--lr", type=float, default=None, help="default 0.02 for sgd, 2e-4 for adamw; a thousandth with --tied, where the lookup's gradient is sqrt(d) times as large")
+    ap.add_argument("--lr", type=float, default=None, help="default 0.02 for sgd, 2e-4 for adamw")
     ap.add_argument("--optimizer", default="sgd", choices=["sgd", "adamw"])
     ap.add_argument("--dtype", default="bf16", choices=["bf16", "f32"])
     ap.add_argument("--logits-cache", action="store_true", help="bf16 only: keep the forward's ratios for the backward")
@@ -149,7 +149,7 @@ def main():
         run, w = iw_grpg_tied, wl.make_tied_workload(spec, seed=0, device="cuda", scale=spec.d ** 0.5, as_served=served_in_8_bits)
     else:
         run, w = iw_grpg, wl.make_workload(spec, seed=0, device="cuda")
-    lr = args.lr if args.lr is not None else (0.02 if args.optimizer == "sgd" else 2e-4) * (1e-3 if args.tied else 1.0)
+    lr = args.lr if args.lr is not None else 0.02 if args.optimizer == "sgd" else 2e-4
     log, summary, _ = run(w, inner_steps=args.inner_steps, lr=lr, logits_cache=args.logits_cache, optimizer=args.optimizer)
     print("step  loss        staleness  clip_frac  max|s|")
     for r in log:
