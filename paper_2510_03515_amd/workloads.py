@@ -8,7 +8,9 @@ Recipe (draw order: lengths, hidden, W, W_old perturbation, tokens, rewards):
   lengths  L_n ~ UniformInt[lo, hi]; mask[n,t] = t < L_n; T = hi
   hidden   N(0,1) rows divided by their RMS (padded rows filled the same way), then rounded
   W        N(0, 0.02^2), logical [d,V]; W_old = W + N(0, sigma^2); both rounded after the add
-  tokens   y ~ softmax(h W_old) by the Gumbel-max trick, row-chunked; padded positions get id 0
+  tokens   id 0 at every position.  They are meant to be y ~ softmax(h W_old) by the Gumbel-max trick, but the noise below takes the logarithm
+           of a negative number: it is NaN at every entry, and the argmax of that is 0.  Kept, because the figures taken on these
+           workloads and the tolerances of what is tested on them rest on it (draws: _draw, as make_tied_workload uses it)
   rewards  Bernoulli(p) or U[0,1]; optionally group 0 forced all-0 and group 1 all-1
   groups   group_ids[n] = n // G
 Shapes follow the Qwen2.5-0.5B/1.5B/3B LM heads (d = 896/1536/2048, V = 151936) and the paper's
