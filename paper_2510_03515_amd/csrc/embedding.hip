@@ -664,7 +664,7 @@ constexpr int64_t FEW_POSITIONS = 131072;
 // One pass over 10 to 12 bits and two of half as many, V = 4096: 8200 positions 23.8 and 30.1 us, 32768 38.2 and 39.1, 65536 62.9 and 59.7.
 constexpr int64_t WIDE_POSITIONS = 32768;
 static_assert(WIDE_POSITIONS <= 256 * SORT_THREADS * FEW_ITEMS && WIDE_POSITIONS <= FEW_POSITIONS, "a block of a wide pass has one round");
-// All passes in one block, and the launches of many.  Ids that many blocks sort in one pass: V = 4096: 2048 positions 18.8 and 19.1 us, 3072 20.1 and 19.6,
+// All passes in one block, and the launches of many.  Ids that many blocks sort in one pass: V = 4096: 2048 positions 18.8 and 19.1 us, 4096 22.7 and 21.2,
 // 8192 29.5 and 22.7; V = 300: 2048 16.4 and 17.4, 4097 21.4 and 19.9.  In two or more: V = 5000: 5120 26.2 and 26.4, 8192 31.8 and 31.2; V = 151936: 4096
 // 30.1 and 32.3, 6144 34.3 and 34.1, 8192 37.3 and 35.2.
 constexpr int64_t ONE_BLOCK_ONE_PASS = 2560, ONE_BLOCK_SORT = 6144;
